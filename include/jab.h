@@ -407,6 +407,93 @@ jab_status jab_omega(int32_t n_layers, int32_t n_probes, const double *curv, int
 jab_status jab_loss_fwd_noalloc(const jab_problem *p, const void *x, const void *w, const jab_quant *q,
                                 const float *a_ref, double *out, void *stream);
 
+/* ------------------------------------------------------------------ the block in use
+ * The entry points below run a quantized block instead of scoring it: the projection on 8-bit
+ * integers, a paged cache of quantized keys and values, and the attention of new tokens over it.  A
+ * batch is the rows of jab_project's y, [batch * seq_len][R]; jab_problem's d_model, heads, head_dim,
+ * dtype, scheme and rope_theta mean what they mean above (group_size is not used), batch * seq_len is
+ * the number of rows, and which rows belong to which sequence is jab_cache_rows'. */
+
+/* Rows onto the symmetric 8-bit grid of eq. quant with one group per row: scale = fp32(max|x| / 127) (1 if
+ * that is 0), code = clip(round_half_even(fp32(x / scale)), -127, 127), every step correctly rounded.
+ * src [rows][d_model] in dtype (activations: a scale per token; weights: per output channel), codes
+ * [rows][d_model] int8, scale [rows] fp32.  A row with an infinite or NaN entry gets scale NaN, codes 0.
+ * Errors: JAB_E_INVALID for NULL or misaligned pointers (16 bytes; scale 4) or rows < 1. */
+jab_status jab_quant_rows(const jab_problem *p, int64_t rows, const void *src, int8_t *codes, float *scale,
+                          void *stream);
+
+/* The fused QKV projection of jab_project on 8-bit integers,
+ *   y[m][n] = sx[m] sw[n] sum_k xq[m][k] wq[n][k],
+ * xq [batch seq_len][d_model] and wq [R][d_model] int8 with their rows' scales sx, sw (jab_quant_rows); y
+ * [batch][seq_len][R] in dtype.  The sum is exact (32-bit integers), the rest fp32: y = dtype(fp32(sum) *
+ * fp32(sx sw)).  Any codes -128..127.  No workspace.  Errors: JAB_E_INVALID for NULL or misaligned pointers (16
+ * bytes; sx 4), JAB_E_UNSUPPORTED for d_model above 131040 (sums past 32 bits). */
+jab_status jab_project_int(const jab_problem *p, const int8_t *xq, const float *sx, const int8_t *wq,
+                           const float *sw, void *y, void *stream);
+
+/* A paged cache of quantized keys and values.  A page holds page_size tokens of every key/value head;
+ * per (token, head) the dh elements are one group of eq. quant's grid at `bits` (4 or 8) in the
+ * problem's scheme: JAB_ASYM as jab_quant_init / jab_quantize form it, with a zero-point; JAB_SYM without,
+ * codes stored as q + q_max.  Layouts (device, the caller's; b = bits, DHB = head_dim b / 8):
+ *   k        [n_pages][n_kv_heads][page_size][DHB] u8
+ *   v        [n_pages][n_kv_heads][page_size / 32][DHB][32] u8 (token t of a block of 32 in column t)
+ *   k_scale, v_scale [n_pages][n_kv_heads][page_size] fp32;  k_zero, v_zero the same in u8 (NULL for JAB_SYM)
+ * At 4 bits byte i of DHB holds element i in its low and element i + head_dim / 2 in its high half.
+ * A (token, head) with an infinite or NaN element, or whose range overflows fp32, is held as NaN (scale NaN).
+ * Alignment: 16 bytes for every buffer. */
+typedef struct {
+    int32_t bits;          /* 4 or 8 */
+    int32_t page_size;     /* 32, 64, 128 or 256 */
+    int32_t n_pages;
+    void *k, *v;
+    float *k_scale, *v_scale;
+    uint8_t *k_zero, *v_zero;
+} jab_cache;
+
+/* Which rows of a batch belong to which sequence, and where its tokens lie.  Device arrays, read when the
+ * kernels run, so a captured graph follows them: sequence s has rows start[s] .. start[s + 1] of the batch,
+ * its new tokens, at positions past[s], past[s] + 1, ...; position t lies in page pages[s][t / page_size].
+ * Pages may be shared between sequences for reading; two rows of one write must not share a place.
+ * Values outside their range are not followed: start is cut to 0 .. batch * seq_len and to be
+ * ascending, past to 0 .. max_pages * page_size; positions past the last column and positions whose
+ * page is not in 0 .. n_pages - 1 are not stored and not seen, and read back as untouched and as 0.
+ * Rows in no sequence are not read, and outputs for them are left as they were. */
+typedef struct {
+    int32_t n_seq, max_pages;
+    int32_t max_new;          /* (host) the most new tokens of a sequence: sizes the launches; a sequence
+                                 with more is still computed in full */
+    const int32_t *pages;     /* [n_seq][max_pages] */
+    const int32_t *past;      /* [n_seq] tokens before the new ones */
+    const int32_t *start;     /* [n_seq + 1] */
+} jab_cache_rows;
+
+/* The key and value columns of y [batch seq_len][R] (jab_project's or jab_project_int's output) into the
+ * cache.  Keys are turned by the rotary embedding at their position first when rope_theta > 0 (angle,
+ * cosine, sine and turn in fp64, rounded to fp32 once).  Errors: JAB_E_INVALID for NULL or misaligned
+ * pointers (y 16 bytes), sizes below 1, bits, page_size or zero-points that do not fit the scheme;
+ * JAB_E_UNSUPPORTED for max_pages * page_size above 2^31 - 512 or n_seq * n_kv_heads above 2^23. */
+jab_status jab_cache_write(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, const void *y,
+                           void *stream);
+
+/* What jab_cache_write with the same rows stored, back as values fp32((code - zero) scale) in dtype: k, v
+ * [batch seq_len][n_kv_heads head_dim] (keys as stored, turned).  A whole sequence: past 0 and its length as its
+ * rows.  Errors as jab_cache_write. */
+jab_status jab_cache_read(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, void *k, void *v,
+                          void *stream);
+
+/* Attention of the batch's queries over the cache: the query columns of y [batch seq_len][R] (turned at their
+ * position when rope_theta > 0), new token i of sequence s seeing positions 0 .. past[s] + i, which
+ * jab_cache_write has stored before; a [batch seq_len][n_heads head_dim] in dtype, head h in columns
+ * h head_dim ...  The softmax, its sums and the output are fp32; queries and softmax weights enter the matrix
+ * products as fp16 (bf16: one part, 2^-11; fp16 and fp32: two, 2^-22), the codes exactly.  A row that sees nothing
+ * gives 0; a query row with an infinite or NaN element gives NaN.  Workspace: jab_attn_cache_workspace bytes (0 when
+ * the key axis is not split), 256-byte aligned.  Errors as jab_cache_write, and JAB_E_WORKSPACE. */
+jab_status jab_attn_cache(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, const void *y, void *a,
+                          void *ws, size_t ws_bytes, void *stream);
+/* Bytes of workspace jab_attn_cache needs, from sizes alone (no device array is read; buffers may still be
+ * NULL); (size_t)-1 for invalid sizes, with jab_last_error. */
+size_t jab_attn_cache_workspace(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r);
+
 const char *jab_status_string(int32_t status);
 const char *jab_last_error(void);
 

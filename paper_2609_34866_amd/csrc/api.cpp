@@ -1172,7 +1172,130 @@ jab_status run_bwd(const jab_problem *p, const void *x, const void *w, const jab
 }
 }  // namespace
 
+namespace {
+// ---------------------------------------------------------------- the block in use
+jab_status check_cache_sizes(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r) {
+    jab_status s = check_problem(p);
+    if (s) return s;
+    JAB_CHECK(c != nullptr && r != nullptr, JAB_E_INVALID, "cache or cache rows are NULL");
+    JAB_CHECK(c->bits == 4 || c->bits == 8, JAB_E_INVALID, "cache bits must be 4 or 8");
+    JAB_CHECK(c->page_size == 32 || c->page_size == 64 || c->page_size == 128 || c->page_size == 256, JAB_E_INVALID,
+              "page_size must be 32, 64, 128 or 256");
+    JAB_CHECK(c->n_pages > 0 && r->n_seq > 0 && r->max_pages > 0 && r->max_new > 0, JAB_E_INVALID,
+              "cache sizes must be positive");
+    JAB_CHECK((int64_t)r->max_pages * c->page_size <= (int64_t)INT32_MAX - 511, JAB_E_UNSUPPORTED,
+              "max_pages * page_size too large for 32-bit positions");
+    JAB_CHECK((int64_t)r->n_seq * p->n_kv_heads <= (1 << 23), JAB_E_UNSUPPORTED, "too many sequences for one launch");
+    return JAB_OK;
+}
+
+jab_status check_cache(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r) {
+    jab_status s = check_cache_sizes(p, c, r);
+    if (s) return s;
+    JAB_CHECK(c->k && aligned(c->k, 16) && c->v && aligned(c->v, 16), JAB_E_INVALID, "cache k / v NULL or not 16-byte aligned");
+    JAB_CHECK(c->k_scale && aligned(c->k_scale, 16) && c->v_scale && aligned(c->v_scale, 16), JAB_E_INVALID,
+              "cache scales NULL or not 16-byte aligned");
+    if (p->scheme == JAB_ASYM)
+        JAB_CHECK(c->k_zero && aligned(c->k_zero, 16) && c->v_zero && aligned(c->v_zero, 16), JAB_E_INVALID,
+                  "cache zero-points are required for JAB_ASYM, 16-byte aligned");
+    else
+        JAB_CHECK(!c->k_zero && !c->v_zero, JAB_E_INVALID, "cache zero-points must be NULL for JAB_SYM");
+    JAB_CHECK(r->pages && aligned(r->pages, 4) && r->past && aligned(r->past, 4) && r->start && aligned(r->start, 4),
+              JAB_E_INVALID, "pages / past / start NULL or misaligned");
+    return JAB_OK;
+}
+
+jab::CacheArgs cache_args(const jab_problem &p, const jab_cache &c, const jab_cache_rows &r) {
+    jab::CacheArgs g;
+    g.M = (int)dims_of(p).M;
+    g.n_heads = p.n_heads; g.n_kv_heads = p.n_kv_heads; g.head_dim = p.head_dim;
+    g.bits = c.bits; g.n_pages = c.n_pages;
+    g.page_shift = 5;
+    while ((1 << g.page_shift) < c.page_size) ++g.page_shift;
+    g.n_seq = r.n_seq; g.max_pages = r.max_pages;
+    g.max_new = std::min(r.max_new, g.M);
+    g.cap = r.max_pages * c.page_size;
+    g.pages = r.pages; g.past = r.past; g.start = r.start;
+    g.k = static_cast<uint8_t *>(c.k); g.v = static_cast<uint8_t *>(c.v);
+    g.k_scale = c.k_scale; g.v_scale = c.v_scale;
+    g.k_zero = c.k_zero; g.v_zero = c.v_zero;
+    for (int j = 0; j < 64; ++j)
+        g.freq[j] = p.rope_theta > 0.f && j < p.head_dim / 2
+                        ? std::pow((double)p.rope_theta, -2.0 * (double)j / (double)p.head_dim) : 0.0;
+    return g;
+}
+}  // namespace
+
 extern "C" {
+
+jab_status jab_quant_rows(const jab_problem *p, int64_t rows, const void *src, int8_t *codes, float *scale,
+                          void *stream) {
+    jab_status s = check_problem(p);
+    if (s) return s;
+    JAB_CHECK(rows > 0, JAB_E_INVALID, "rows must be positive");
+    JAB_CHECK(src && aligned(src, 16) && codes && aligned(codes, 16), JAB_E_INVALID, "src / codes NULL or not 16-byte aligned");
+    JAB_CHECK(scale && aligned(scale, 4), JAB_E_INVALID, "scale is NULL or misaligned");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    JAB_RUN(JAB_KT_QUANT, st, "row quantizer",
+            jab::launch_quant_rows(p->dtype, rows, p->d_model, src, codes, scale, st));
+    return JAB_OK;
+}
+
+jab_status jab_project_int(const jab_problem *p, const int8_t *xq, const float *sx, const int8_t *wq, const float *sw,
+                           void *y, void *stream) {
+    jab_status s = check_problem(p);
+    if (s) return s;
+    JAB_CHECK(p->d_model <= 131040, JAB_E_UNSUPPORTED, "d_model too large for 32-bit sums of 8-bit products");
+    JAB_CHECK(xq && aligned(xq, 16) && wq && aligned(wq, 16), JAB_E_INVALID, "xq / wq NULL or not 16-byte aligned");
+    JAB_CHECK(sx && aligned(sx, 4) && sw && aligned(sw, 16), JAB_E_INVALID, "sx / sw NULL or misaligned");
+    JAB_CHECK(y && aligned(y, 16), JAB_E_INVALID, "y NULL or not 16-byte aligned");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const Dims D = dims_of(*p);
+    JAB_RUN(JAB_KT_GEMM, st, "integer projection",
+            jab::launch_project_int(p->dtype, xq, sx, wq, sw, y, (int)D.M, (int)D.R, (int)D.d, st));
+    return JAB_OK;
+}
+
+jab_status jab_cache_write(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, const void *y, void *stream) {
+    jab_status s = check_cache(p, c, r);
+    if (s) return s;
+    JAB_CHECK(y && aligned(y, 16), JAB_E_INVALID, "y NULL or not 16-byte aligned");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const jab::CacheArgs g = cache_args(*p, *c, *r);
+    JAB_RUN(JAB_KT_QUANT, st, "cache write", jab::launch_cache_write(p->dtype, g, y, dims_of(*p).R, st));
+    return JAB_OK;
+}
+
+jab_status jab_cache_read(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, void *k, void *v, void *stream) {
+    jab_status s = check_cache(p, c, r);
+    if (s) return s;
+    JAB_CHECK(k && aligned(k, 16) && v && aligned(v, 16), JAB_E_INVALID, "k / v NULL or not 16-byte aligned");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const jab::CacheArgs g = cache_args(*p, *c, *r);
+    JAB_RUN(JAB_KT_MISC, st, "cache read", jab::launch_cache_read(p->dtype, g, k, v, st));
+    return JAB_OK;
+}
+
+size_t jab_attn_cache_workspace(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r) {
+    if (check_cache_sizes(p, c, r) != JAB_OK) return (size_t)-1;
+    return jab::attn_cache_ws_bytes(cache_args(*p, *c, *r));
+}
+
+jab_status jab_attn_cache(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, const void *y, void *a, void *ws,
+                          size_t ws_bytes, void *stream) {
+    jab_status s = check_cache(p, c, r);
+    if (s) return s;
+    JAB_CHECK(y && aligned(y, 16) && a && aligned(a, 16), JAB_E_INVALID, "y / a NULL or not 16-byte aligned");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const jab::CacheArgs g = cache_args(*p, *c, *r);
+    const size_t need = jab::attn_cache_ws_bytes(g);
+    if (need) {
+        JAB_CHECK(ws && aligned(ws, 256), JAB_E_INVALID, "workspace is NULL or not 256-byte aligned");
+        JAB_CHECK(ws_bytes >= need, JAB_E_WORKSPACE, "workspace too small for jab_attn_cache");
+    }
+    JAB_RUN(JAB_KT_ATTN, st, "attention over the cache", jab::launch_attn_cache(p->dtype, g, y, dims_of(*p).R, a, ws, st));
+    return JAB_OK;
+}
 
 jab_status jab_set_bwd_ds_limit(size_t max_bytes) {
     g_ds_limit = max_bytes;

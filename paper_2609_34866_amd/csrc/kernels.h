@@ -245,4 +245,29 @@ hipError_t launch_rope_rows(int dtype, const float *src, int64_t lds, void *dst,
                             int heads, int dh, const float2 *tab, hipStream_t st);
 hipError_t launch_rope_cols(int dtype, void *yt, int64_t ldt, int64_t ncols, int T, int heads, int dh,
                             const float2 *tab, bool inverse, hipStream_t st);
+// ---- 8-bit projection (gemm_int.hip): rows of `cols` values (a multiple of 32) onto the symmetric 8-bit grid, one
+// scale per row; y[m][n] = sx[m] sw[n] sum_k xq[m][k] wq[n][k] in dtype, N a multiple of 16, K of 32, K < 2^17
+hipError_t launch_quant_rows(int dtype, int64_t rows, int cols, const void *src, int8_t *codes, float *scale,
+                             hipStream_t st);
+hipError_t launch_project_int(int dtype, const int8_t *xq, const float *sx, const int8_t *wq, const float *sw, void *y,
+                              int M, int N, int K, hipStream_t st);
+// ---- paged cache of quantized keys and values (cache.h has the layout)
+struct CacheArgs {
+    int M;                              // rows of the batch
+    int n_heads, n_kv_heads, head_dim;
+    int bits, page_shift, n_pages;      // page_size = 1 << page_shift
+    int n_seq, max_pages, max_new;
+    int cap;                            // tokens of a sequence: max_pages * page_size
+    const int32_t *pages, *past, *start;
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    uint8_t *k_zero, *v_zero;           // NULL: symmetric grid
+    double freq[64];                    // rotary embedding: radians per position of pair j; freq[0] = 0: none
+};
+// y [M][ldy] in dtype: query, key and value columns; k_out, v_out [M][n_kv_heads head_dim]
+hipError_t launch_cache_write(int dtype, const CacheArgs &g, const void *y, int64_t ldy, hipStream_t st);
+hipError_t launch_cache_read(int dtype, const CacheArgs &g, void *k_out, void *v_out, hipStream_t st);
+// a [M][n_heads head_dim] in dtype; ws: attn_cache_ws_bytes(g) (may be 0)
+size_t attn_cache_ws_bytes(const CacheArgs &g);
+hipError_t launch_attn_cache(int dtype, const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st);
 }  // namespace jab

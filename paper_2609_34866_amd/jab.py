@@ -66,6 +66,17 @@ class SteConfig(ctypes.Structure):
                 ("adam_eps", ctypes.c_float), ("scale_floor", ctypes.c_float), ("lambda_kl", ctypes.c_float)]
 
 
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("bits", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("k_zero", ctypes.c_void_p), ("v_zero", ctypes.c_void_p)]
+
+
+class _CacheRowsStruct(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("pages", ctypes.c_void_p), ("past", ctypes.c_void_p), ("start", ctypes.c_void_p)]
+
+
 def problem(batch, seq_len, d_model, n_heads, n_kv_heads, head_dim, group_size, dtype,
             scheme: int = ASYM, rope_theta: float = 0.0) -> Problem:
     code = _DTYPE_CODE[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
@@ -90,7 +101,7 @@ def lib() -> ctypes.CDLL:
         raise RuntimeError(f"libjab.so is not built ({LIB_PATH}); run __graft_entry__.build()")
     L = ctypes.CDLL(LIB_PATH)
     vp, sz, i32, P = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.POINTER(Problem)
-    Q = ctypes.POINTER(Quant)
+    Q, C, R = ctypes.POINTER(Quant), ctypes.POINTER(_CacheStruct), ctypes.POINTER(_CacheRowsStruct)
     sig = {
         "jab_workspace_size": (sz, [P, i32, i32]),
         "jab_quant_init": (i32, [P, vp, vp, vp, vp, vp]),
@@ -111,6 +122,12 @@ def lib() -> ctypes.CDLL:
         "jab_ste_stats_len": (i32, [i32, i32]),
         "jab_ste_finetune": (i32, [P, ctypes.POINTER(SteConfig), vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                    vp, vp, vp, vp, vp, sz, vp]),
+        "jab_quant_rows": (i32, [P, ctypes.c_int64, vp, vp, vp, vp]),
+        "jab_project_int": (i32, [P, vp, vp, vp, vp, vp, vp]),
+        "jab_cache_write": (i32, [P, C, R, vp, vp]),
+        "jab_cache_read": (i32, [P, C, R, vp, vp, vp]),
+        "jab_attn_cache": (i32, [P, C, R, vp, vp, vp, sz, vp]),
+        "jab_attn_cache_workspace": (sz, [P, C, R]),
         "jab_status_string": (ctypes.c_char_p, [i32]),
         "jab_last_error": (ctypes.c_char_p, []),
         "jab_set_bwd_ds_limit": (i32, [ctypes.c_size_t]),
@@ -127,7 +144,9 @@ def lib() -> ctypes.CDLL:
 EXPORTED = ("jab_workspace_size", "jab_quant_init", "jab_quantize", "jab_attn_ref", "jab_loss_fwd",
             "jab_loss_fwd_noalloc",
             "jab_attn_ref_kl", "jab_loss_fwd_kl", "jab_loss_sweep", "jab_loss_bwd", "jab_project",
-            "jab_allocate", "jab_omega", "jab_curvature", "jab_fisher", "jab_loss_bwd_kl", "jab_ste_stats_len", "jab_ste_finetune", "jab_status_string", "jab_last_error", "jab_set_bwd_ds_limit", "jab_timing_enable",
+            "jab_allocate", "jab_omega", "jab_curvature", "jab_fisher", "jab_loss_bwd_kl", "jab_ste_stats_len", "jab_ste_finetune",
+            "jab_quant_rows", "jab_project_int", "jab_cache_write", "jab_cache_read", "jab_attn_cache",
+            "jab_attn_cache_workspace", "jab_status_string", "jab_last_error", "jab_set_bwd_ds_limit", "jab_timing_enable",
             "jab_timing_read")
 ALLOC_GREEDY, ALLOC_PARETO = 0, 1
 TRACE_BLOCK, TRACE_UNIT = 0, 1
@@ -376,6 +395,151 @@ def loss_bwd_kl(p: Problem, x, w, bits, scale, zero, a_ref, qk_ref, lse_ref, gsc
                                  _ptr(lse_ref), ctypes.cast(g, ctypes.c_void_p), float(lambda_kl), _ptr(out),
                                  _ptr(dw), _ptr(ds), _ptr(ws), ws.numel(), _stream()))
     return out, dw, ds
+
+
+# --------------------------------------------------------------------------- the block in use
+def _arg(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device=None) -> int:
+    """The address of a contiguous tensor of this dtype and shape on this device (None: the current one)."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise JabError(JAB_E_INVALID, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not "
+                                      f"{t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ' with strides'}")
+    if t.device.type != "cuda" or t.device.index != (torch.cuda.current_device() if device is None else device):
+        raise JabError(JAB_E_INVALID, f"{name} is on {t.device}, not on the current GPU")
+    return t.data_ptr()
+
+
+def quant_rows(p: Problem, src: torch.Tensor, codes: Optional[torch.Tensor] = None,
+               scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows of d_model values (any leading dimensions) onto the symmetric 8-bit grid, a scale per row ->
+    (codes int8 of src's shape, scale fp32 of its leading dimensions)."""
+    if src.dim() < 1 or src.shape[-1] != p.d_model:
+        raise JabError(JAB_E_INVALID, f"src must have rows of d_model = {p.d_model} values, not shape {tuple(src.shape)}")
+    sp = _arg("src", src, p.torch_dtype, src.shape)
+    if codes is None:
+        codes = torch.empty(src.shape, dtype=torch.int8, device=src.device)
+    if scale is None:
+        scale = torch.empty(src.shape[:-1], dtype=torch.float32, device=src.device)
+    _check(lib().jab_quant_rows(ctypes.byref(p), src.numel() // p.d_model, sp,
+                                _arg("codes", codes, torch.int8, src.shape),
+                                _arg("scale", scale, torch.float32, src.shape[:-1]), _stream()))
+    return codes, scale
+
+
+def project_int(p: Problem, xq: torch.Tensor, sx: torch.Tensor, wq: torch.Tensor, sw: torch.Tensor,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The fused projection on 8-bit integers: codes xq [B][T][d_model], wq [R][d_model] and their rows'
+    scales (quant_rows) -> y [B][T][R]."""
+    B, T, d = p.batch, p.seq_len, p.d_model
+    if out is None:
+        out = torch.empty((B, T, p.rows), dtype=p.torch_dtype, device=xq.device)
+    _check(lib().jab_project_int(ctypes.byref(p), _arg("xq", xq, torch.int8, (B, T, d)),
+                                 _arg("sx", sx, torch.float32, (B, T)), _arg("wq", wq, torch.int8, (p.rows, d)),
+                                 _arg("sw", sw, torch.float32, (p.rows,)),
+                                 _arg("out", out, p.torch_dtype, (B, T, p.rows)), _stream()))
+    return out
+
+
+class Cache:
+    """The paged cache of quantized keys and values of one block: the caller's tensors (jab_cache has the layouts)."""
+
+    def __init__(self, p: Problem, bits: int, page_size: int, k, v, k_scale, v_scale, k_zero=None, v_zero=None):
+        if bits not in (4, 8) or page_size not in (32, 64, 128, 256):
+            raise JabError(JAB_E_INVALID, "bits must be 4 or 8 and page_size 32, 64, 128 or 256")
+        n, h, dhb = k.shape[0], p.n_kv_heads, p.head_dim * bits // 8
+        if (p.scheme == ASYM) != (k_zero is not None) or (k_zero is None) != (v_zero is None):
+            raise JabError(JAB_E_INVALID, "zero-points go with the asymmetric scheme")
+        self.tensors = (k, v, k_scale, v_scale, k_zero, v_zero)      # kept alive with the struct's addresses
+        self.geometry = (h, p.head_dim, p.scheme)
+        self.device = k.device.index
+        dev = self.device
+        rows = (n, h, page_size)
+        self.struct = _CacheStruct(
+            bits, page_size, n, _arg("k", k, torch.uint8, rows + (dhb,), dev),
+            _arg("v", v, torch.uint8, (n, h, page_size // 32, dhb, 32), dev),
+            _arg("k_scale", k_scale, torch.float32, rows, dev), _arg("v_scale", v_scale, torch.float32, rows, dev),
+            None if k_zero is None else _arg("k_zero", k_zero, torch.uint8, rows, dev),
+            None if v_zero is None else _arg("v_zero", v_zero, torch.uint8, rows, dev))
+
+    @classmethod
+    def empty(cls, p: Problem, bits: int, page_size: int, n_pages: int, device="cuda") -> "Cache":
+        """A cache of n_pages unwritten pages."""
+        h, dhb = p.n_kv_heads, p.head_dim * bits // 8
+        rows = (n_pages, h, page_size)
+
+        def buf(shape, dtype):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        z = p.scheme == ASYM
+        return cls(p, bits, page_size, buf(rows + (dhb,), torch.uint8),
+                   buf((n_pages, h, page_size // 32, dhb, 32), torch.uint8), buf(rows, torch.float32),
+                   buf(rows, torch.float32), buf(rows, torch.uint8) if z else None, buf(rows, torch.uint8) if z else None)
+
+
+class CacheRows:
+    """Which rows of a batch belong to which sequence (jab_cache_rows): pages int32 [n_seq][max_pages], past
+    int32 [n_seq], start int32 [n_seq + 1], and the most new tokens of a sequence."""
+
+    def __init__(self, pages: torch.Tensor, past: torch.Tensor, start: torch.Tensor, max_new: int):
+        if pages.dim() != 2:
+            raise JabError(JAB_E_INVALID, "pages must be [n_seq][max_pages]")
+        n = pages.shape[0]
+        self.device = pages.device.index
+        dev = self.device
+        self.tensors = (pages, past, start)
+        self.struct = _CacheRowsStruct(n, pages.shape[1], int(max_new), _arg("pages", pages, torch.int32, pages.shape, dev),
+                                       _arg("past", past, torch.int32, (n,), dev),
+                                       _arg("start", start, torch.int32, (n + 1,), dev))
+
+
+def _cache_call(p: Problem, cache: Cache, rows: CacheRows):
+    if cache.geometry != (p.n_kv_heads, p.head_dim, p.scheme):
+        raise JabError(JAB_E_INVALID, "the cache was laid out for other heads or another scheme")
+    if cache.device != torch.cuda.current_device() or rows.device != cache.device:
+        raise JabError(JAB_E_INVALID, "the cache and its rows must be on the current GPU")
+    return ctypes.byref(p), ctypes.byref(cache.struct), ctypes.byref(rows.struct)
+
+
+def cache_write(p: Problem, cache: Cache, rows: CacheRows, y: torch.Tensor) -> None:
+    """The key (turned by the rotary embedding) and value columns of y [B][T][R] into the cache."""
+    a = _cache_call(p, cache, rows)
+    _check(lib().jab_cache_write(*a, _arg("y", y, p.torch_dtype, (p.batch, p.seq_len, p.rows)), _stream()))
+
+
+def cache_read(p: Problem, cache: Cache, rows: CacheRows, k: Optional[torch.Tensor] = None,
+               v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """What cache_write stored for these rows -> (k, v) [B][T][n_kv_heads * head_dim] in the dtype."""
+    a = _cache_call(p, cache, rows)
+    shape = (p.batch, p.seq_len, p.n_kv_heads * p.head_dim)
+    dev = cache.tensors[0].device
+    if k is None:
+        k = torch.empty(shape, dtype=p.torch_dtype, device=dev)
+    if v is None:
+        v = torch.empty(shape, dtype=p.torch_dtype, device=dev)
+    _check(lib().jab_cache_read(*a, _arg("k", k, p.torch_dtype, shape), _arg("v", v, p.torch_dtype, shape), _stream()))
+    return k, v
+
+
+def attn_cache_workspace(p: Problem, cache: Cache, rows: CacheRows) -> torch.Tensor:
+    """The workspace attn_cache needs for this cache and these rows' sizes (possibly empty)."""
+    n = lib().jab_attn_cache_workspace(ctypes.byref(p), ctypes.byref(cache.struct), ctypes.byref(rows.struct))
+    if n == ctypes.c_size_t(-1).value:
+        raise JabError(JAB_E_INVALID, lib().jab_last_error().decode())
+    return torch.empty(n, dtype=torch.uint8, device=cache.tensors[0].device)
+
+
+def attn_cache(p: Problem, cache: Cache, rows: CacheRows, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of y's query columns over the cache -> [B][T][n_heads * head_dim] in the dtype."""
+    a = _cache_call(p, cache, rows)
+    shape = (p.batch, p.seq_len, p.n_heads * p.head_dim)
+    if out is None:
+        out = torch.empty(shape, dtype=p.torch_dtype, device=y.device)
+    if ws is None:
+        ws = attn_cache_workspace(p, cache, rows)
+    _check(lib().jab_attn_cache(*a, _arg("y", y, p.torch_dtype, (p.batch, p.seq_len, p.rows)),
+                                _arg("out", out, p.torch_dtype, shape),
+                                _arg("ws", ws, torch.uint8, ws.shape), ws.numel(), _stream()))
+    return out
 
 
 CURVATURE_FORMS = ("t_Q", "t_K", "t_V", "pooled", "h_QQ", "h_KK", "h_VV")
