@@ -184,7 +184,7 @@ def _own(s):
     p = h["p"]
     if c["op"] == "proj":
         xq, sx = jab.quant_rows(p, s["x"])
-        return jab.project_int(p, xq, sx, s["wq"], s["sw"]), sx
+        return jab.project_int(p, xq, sx, s["wq"], s["sw"]), sx[0]
     if c["op"] == "cache":
         jab.cache_write(p, h["cache"], h["rows"], s["y"])
         k, v = jab.cache_read(p, h["cache"], h["rows"])
