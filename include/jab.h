@@ -471,7 +471,8 @@ typedef struct {
  * cache.  Keys are turned by the rotary embedding at their position first when rope_theta > 0 (angle,
  * cosine, sine and turn in fp64, rounded to fp32 once).  Errors: JAB_E_INVALID for NULL or misaligned
  * pointers (y 16 bytes), sizes below 1, bits, page_size or zero-points that do not fit the scheme;
- * JAB_E_UNSUPPORTED for max_pages * page_size above 2^31 - 512 or n_seq * n_kv_heads above 2^23. */
+ * JAB_E_UNSUPPORTED for max_pages * page_size or batch * seq_len * n_heads / n_kv_heads above 2^31 - 512, or
+ * n_seq * n_kv_heads above 2^23. */
 jab_status jab_cache_write(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, const void *y,
                            void *stream);
 

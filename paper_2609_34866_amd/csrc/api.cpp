@@ -1185,6 +1185,8 @@ jab_status check_cache_sizes(const jab_problem *p, const jab_cache *c, const jab
               "cache sizes must be positive");
     JAB_CHECK((int64_t)r->max_pages * c->page_size <= (int64_t)INT32_MAX - 511, JAB_E_UNSUPPORTED,
               "max_pages * page_size too large for 32-bit positions");
+    JAB_CHECK(dims_of(*p).M * (p->n_heads / p->n_kv_heads) <= INT32_MAX - 511, JAB_E_UNSUPPORTED,
+              "too many query rows of one key/value head for 32-bit indices");
     JAB_CHECK((int64_t)r->n_seq * p->n_kv_heads <= (1 << 23), JAB_E_UNSUPPORTED, "too many sequences for one launch");
     return JAB_OK;
 }

@@ -33,6 +33,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LAZY = 8.f;             // log2 of what a score may exceed the reference by
 constexpr int WUP = 6;                  // log2 of the weights' extra scale: p sv <= 2^(8 + 6) in fp16
 constexpr int EMIN = -125;
+constexpr int NOWHERE = INT32_MAX - 63; // a key past every position
 
 // two codes of a word as fp16 integers, 1024 + code: bytes 0, 1 (hi false) or 2, 3
 __device__ inline f16x2 biased(uint32_t w, bool hi) {
@@ -53,428 +54,615 @@ __device__ inline f32x4 mma16(f16x8 a, f16x8 b, f32x4 c) {
 }
 __device__ inline float pow2i(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
-// what a lane reads of a block of 32 tokens
+// The bytes of a block of 32 tokens that one lane supplies to the products, eight consecutive ones at a time
+// ("units"): a unit is one operand at 8 bits, two at 4 bits (low and high halves), half of one at head_dim 16.
 template <int DH, int BITS>
-struct Raw {
+struct Lay {
     static constexpr int DHB = DH * BITS / 8;
-    static constexpr int KB = DHB / 4 < 8 ? 8 : DHB / 4;   // key bytes of a lane and tile
-    static constexpr int NV = DHB / 16 < 1 ? 1 : DHB / 16; // 16-row tiles of value bytes
-    uint32_t k[2][KB / 4];
-    u32x2 v[NV];
-    f32x4 ks[2], vs[2];
-    int kz[2];
-    u32x2 vz;
-    bool in;                                               // the block's page exists
+    static constexpr int KS = DH / 32 < 1 ? 1 : DH / 32;                 // steps of 32 along the head
+    static constexpr int NT = DH / 16;                                   // 16-row tiles of O^T
+    static constexpr int KU = DH < 64 ? 1 : KS * BITS / 8;               // key units of a 16-key tile
+    static constexpr int VU = DH < 64 ? 1 : NT * BITS / 8;               // value units
+    // key row m of tile t
+    static __device__ inline int key(int t, int l16) { return 8 * (l16 >> 2) + 4 * t + (l16 & 3); }
+    // byte of key unit u in its row; groups 2 and 3 of head_dim 16 meet zeros of the query
+    static __device__ inline int kbyte(int u, int grp) {
+        if constexpr (DHB >= 64) return 64 * (u >> 1) + 16 * grp + 8 * (u & 1);
+        else if constexpr (DHB == 32) return 8 * grp;
+        else if constexpr (DHB == 16) return 8 * (grp & 1);
+        else return 0;
+    }
+    // byte row of value unit u
+    static __device__ inline int vrow(int u, int l16) { return 16 * u + (DHB >= 16 ? l16 : l16 & 7); }
+    // first element along the head of step ks (the query's order)
+    static __device__ inline int dim(int ks, int grp) {
+        if constexpr (DH == 128) return 64 * (ks >> 1) + 16 * grp + 8 * (ks & 1);
+        else if constexpr (DH == 64) return BITS == 8 ? 16 * grp + 8 * ks : 32 * ks + 8 * grp;
+        else return 8 * grp;
+    }
+    // the operand of step ks (tile t) from the units' bytes
+    static __device__ inline f16x8 kop(const u32x2 (&k)[KU], int ks, int grp, const f16x2 (&z)[4]) {
+        if constexpr (BITS == 8) return codes8(k[ks][0], k[ks][1], z);
+        else {
+            const int u = DH < 64 ? 0 : ks % KU, sft = DH < 64 ? (grp & 1) * 4 : ks < KU ? 0 : 4;
+            return codes8((k[u][0] >> sft) & 0x0F0F0F0Fu, (k[u][1] >> sft) & 0x0F0F0F0Fu, z);
+        }
+    }
+    static __device__ inline f16x8 vop(const u32x2 (&v)[VU], int t, int l16, const f16x2 (&z)[4]) {
+        if constexpr (BITS == 8) return codes8(v[t][0], v[t][1], z);
+        else {
+            const int u = DH < 64 ? 0 : t % VU, sft = DH < 64 ? (l16 >> 3) * 4 : t < VU ? 0 : 4;
+            return codes8((v[u][0] >> sft) & 0x0F0F0F0Fu, (v[u][1] >> sft) & 0x0F0F0F0Fu, z);
+        }
+    }
 };
 
-template <int DH, int BITS>
-__device__ inline void load_block(const CacheArgs &g, int s, int h, int blk, int lane, Raw<DH, BITS> &r) {
-    typedef Raw<DH, BITS> R;
-    const int l16 = lane & 15, grp = lane >> 4;
+// from a wave-uniform base and a lane's byte offset
+template <typename T>
+__device__ inline T ldu(const uint8_t *base, uint32_t off) { return *reinterpret_cast<const T *>(base + off); }
+
+// where block blk of a sequence lies: its first slot, or -1
+__device__ inline int64_t block_slot(const CacheArgs &g, int s, int h, int blk) {
     const int page = __builtin_amdgcn_readfirstlane(page_of(g, s, blk * 32));
-    r.in = page >= 0;
-    const int64_t slot = (((int64_t)max(page, 0) * g.n_kv_heads + h) << g.page_shift) +
-                         ((blk * 32) & ((1 << g.page_shift) - 1));
-    const uint8_t *kb = g.k + slot * R::DHB, *vb = g.v + slot * R::DHB;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int key = 8 * (l16 >> 2) + 4 * t + (l16 & 3);
-        const uint8_t *row = kb + key * R::DHB;
-        if constexpr (R::KB >= 16) {
-#pragma unroll
-            for (int i = 0; i < R::KB / 16; ++i) {
-                const u32x4 q = *reinterpret_cast<const u32x4 *>(row + 64 * i + 16 * grp);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) r.k[t][4 * i + c] = q[c];
-            }
-        } else {                                           // DH 16: groups 2 and 3 meet zeros of the query
-            const u32x2 q = *reinterpret_cast<const u32x2 *>(row + (R::DHB >= 32 ? 8 * grp : R::DHB >= 16 ? 8 * (grp & 1) : 0));
-            r.k[t][0] = q[0];
-            r.k[t][1] = q[1];
-        }
-        if (g.k_zero) r.kz[t] = g.k_zero[slot + key];
-    }
-#pragma unroll
-    for (int i = 0; i < R::NV; ++i)
-        r.v[i] = *reinterpret_cast<const u32x2 *>(vb + (16 * i + (R::DHB >= 16 ? l16 : l16 & 7)) * 32 + 8 * grp);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        r.ks[i] = *reinterpret_cast<const f32x4 *>(g.k_scale + slot + 8 * grp + 4 * i);
-        r.vs[i] = *reinterpret_cast<const f32x4 *>(g.v_scale + slot + 8 * grp + 4 * i);
-    }
-    if (g.v_zero) r.vz = *reinterpret_cast<const u32x2 *>(g.v_zero + slot + 8 * grp);
+    if (page < 0) return -1;
+    return (((int64_t)page * g.n_kv_heads + h) << g.page_shift) + ((blk * 32) & ((1 << g.page_shift) - 1));
 }
 
-// SPLIT: the four waves of a workgroup share 16 RT rows and deal out the key blocks; else each wave has 16 RT
-// rows of its own
-template <int DT, int DH, int BITS, int RT, bool SPLIT>
-struct AttnCfg {
+// The softmax state of 16 RT rows of one wave: lane (l16, grp) holds row l16 of each tile, of O^T its elements
+// 16 t + 4 grp .. + 3, of l the part of its own keys.
+template <int DT, int DH, int BITS, int RT>
+struct Wave {
     static constexpr int NP = DT == BF16 ? 1 : 2;          // fp16 parts of queries and weights
-    static constexpr int KS = DH / 32 < 1 ? 1 : DH / 32;   // steps of 32 along the head
-    static constexpr int NT = DH / 16;                     // 16-row tiles of O^T
-    static constexpr int ROWS = 16 * RT * (SPLIT ? 1 : 4); // rows of a workgroup
-    static constexpr int QP = DH < 32 ? 40 : DH + 8;       // fp16 per row of queries in LDS (padding against conflicts)
-    static constexpr size_t Q_LDS = (size_t)NP * 16 * QP * 2 * (SPLIT ? RT : 4);
-    static constexpr size_t O_LDS = SPLIT ? (size_t)4 * 16 * RT * (DH + 4) * 4 : 0;
-    static constexpr size_t LDS = Q_LDS > O_LDS ? Q_LDS : O_LDS;
-};
+    typedef Lay<DH, BITS> L;
+    f16x8 qf[RT][NP][L::KS];
+    float fs[RT];                                          // score scale (exp2 units)
+    int lim[RT], lo_lim, hi_lim;                           // last position seen: by this lane's rows, least and most of the wave
+    float m[RT], nm[RT], l[RT];
+    f32x4 o[RT][L::NT];
+    int E;
+    float Rmax, rinv;                                      // 2^E, 2^-E
 
-template <int DT>
-__device__ inline void store4(typename Mma<DT>::elem *p, f32x4 v) {
-    if constexpr (DT == F32) *reinterpret_cast<f32x4 *>(p) = v;
-    else *reinterpret_cast<u32x2 *>(p) = u32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
-}
-
-// grid: x = (sequence, key/value head, split), y = row tiles (dealt out)
-template <int DT, int DH, int BITS, int RT, bool SPLIT>
-__global__ __launch_bounds__(256) void attn_cache_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy,
-                                                         void *__restrict__ av, float *__restrict__ part, int n_split) {
-    typedef AttnCfg<DT, DH, BITS, RT, SPLIT> S;
-    typedef typename Mma<DT>::elem elem;
-    constexpr int HALF = DH / 2, QMID = (1 << (BITS - 1)) - 1;
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float rowf[SPLIT ? 16 * RT : 64];           // per row: score scale (log2 units)
-    __shared__ float mlE[4][16 * RT][2];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int l16 = lane & 15, grp = lane >> 4;
-    const int split = blockIdx.x % n_split, sh = blockIdx.x / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
-    const SeqRows sr = seq_rows(g, s);
-    const int G = g.n_heads / g.n_kv_heads;
-    const int64_t n_rows = (int64_t)sr.n * G;
-    const int len = (int)min((int64_t)sr.past + sr.n, (int64_t)g.cap), n_blk = (len + 31) >> 5;
-    const int b0 = (int)((int64_t)n_blk * split / n_split), b1 = (int)((int64_t)n_blk * (split + 1) / n_split);
-
-    for (int64_t tile = blockIdx.y; tile * S::ROWS < n_rows; tile += gridDim.y) {
-        const int64_t row0 = tile * S::ROWS + (SPLIT ? 0 : wave * 16 * RT);     // this wave's first row
-        // ---- queries: turned, scaled, split in fp16 parts, through LDS into operands
-        f16x8 qf[RT][S::NP][S::KS];
-        float fs[RT];                                      // the score scale of this lane's row
-        int lim[RT];                                       // last position that it sees (no row: none)
-        _Float16 *ql = reinterpret_cast<_Float16 *>(smem) + (SPLIT ? 0 : wave * S::NP * 16 * S::QP);
-        auto prep = [&](int64_t row, int slot, int fslot, int np_stride) {      // one row by one wave
-            float x0 = 0.f, x1 = 0.f;
-            const bool live = lane < HALF && row < n_rows;
-            const int i = live ? (int)(row / G) : 0;
-            if (live) {
-                const elem *q = static_cast<const elem *>(yv) + (int64_t)(sr.row + i) * ldy +
-                                ((int64_t)h * G + row % G) * DH + lane;
-                x0 = to_f32<DT>(q[0]);
-                x1 = to_f32<DT>(q[HALF]);
-            }
-            uint32_t mx = max(__builtin_bit_cast(uint32_t, x0) & 0x7FFFFFFFu, __builtin_bit_cast(uint32_t, x1) & 0x7FFFFFFFu);
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, off, 64));
-            const int e = min(max((int)(mx >> 23) - 127, -100), 127);           // exponent of the largest element
-            const float up = pow2i(max(3 - e, -126));
-            if (g.freq[0] != 0.0 && live) {
-                // turns to the nearest quarter of a cycle in fp64, the rest in fp32
-                const double cyc = (double)(sr.past + i) * g.freq[lane] * 0.15915494309189535;
-                float sn, cs;
-                sincospif((float)(2.0 * (cyc - rint(cyc))), &sn, &cs);
-                const float a = x0 * up, b = x1 * up;
-                x0 = a * cs - b * sn;
-                x1 = b * cs + a * sn;
-            } else {
-                x0 *= up;
-                x1 *= up;
-            }
-            const bool fine = mx < 0x7F800000u;
-            if (lane < HALF) {
-#pragma unroll
-                for (int p = 0; p < S::NP; ++p) {
-                    const _Float16 a = fine ? (_Float16)x0 : (_Float16)0.f, b = fine ? (_Float16)x1 : (_Float16)0.f;
-                    ql[p * np_stride + slot * S::QP + lane] = a;
-                    ql[p * np_stride + slot * S::QP + lane + HALF] = b;
-                    x0 -= (float)a;
-                    x1 -= (float)b;
-                }
-            }
-            if constexpr (DH < 32)
-                if (lane >= DH && lane < 32)
-                    for (int p = 0; p < S::NP; ++p) ql[p * np_stride + slot * S::QP + lane] = (_Float16)0.f;
-            // exp2 units per product unit, the power of two taken back; a row that is not finite gives NaN
-            const float f = LOG2E / sqrtf((float)DH) / up;
-            if (lane == 0) rowf[fslot] = fine ? f : __builtin_nanf("");
-        };
-        auto fetch = [&](int rt, int slot0, int np_stride) {
-            // element order along the head, matching a lane's key bytes
-#pragma unroll
-            for (int p = 0; p < S::NP; ++p)
-#pragma unroll
-                for (int ks = 0; ks < S::KS; ++ks) {
-                    int d;
-                    if constexpr (DH == 128) d = 64 * (ks >> 1) + 16 * grp + 8 * (ks & 1);
-                    else if constexpr (DH == 64) d = BITS == 8 ? 16 * grp + 8 * ks : 32 * ks + 8 * grp;
-                    else d = 8 * grp;
-                    qf[rt][p][ks] = *reinterpret_cast<const f16x8 *>(ql + p * np_stride + (slot0 + l16) * S::QP + d);
-                }
-        };
-        __syncthreads();                                   // LDS of the tile before
-        if constexpr (SPLIT) {
-            for (int r = wave; r < 16 * RT; r += 4) prep(row0 + r, r, r, 16 * RT * S::QP);
-            __syncthreads();
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                fetch(rt, 16 * rt, 16 * RT * S::QP);
-                fs[rt] = rowf[16 * rt + l16];
-            }
-        } else {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                for (int r = 0; r < 16; ++r) prep(row0 + 16 * rt + r, r, wave * 16 + r, 16 * S::QP);
-                __syncthreads();
-                fetch(rt, 0, 16 * S::QP);
-                fs[rt] = rowf[wave * 16 + l16];
-                __syncthreads();
-            }
-        }
-        // the first and last position that a row of the wave sees last; rows that do not exist count as the last
-        int lo_lim = INT32_MAX, hi_lim = -1;
+    __device__ inline void limits(const CacheArgs &g, const SeqRows &sr, int G, int row0, int n_rows, int l16) {
+        lo_lim = INT32_MAX;
+        hi_lim = -1;
         if (row0 < n_rows) {
-            lo_lim = min(sr.past + (int)(row0 / G), g.cap - 1);
-            hi_lim = min(sr.past + (int)((min(row0 + 16 * RT, n_rows) - 1) / G), g.cap - 1);
+            lo_lim = min(sr.past + row0 / G, g.cap - 1);
+            hi_lim = min(sr.past + (min(row0 + 16 * RT, n_rows) - 1) / G, g.cap - 1);
         }
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int64_t row = row0 + 16 * rt + l16;
-            lim[rt] = row < n_rows ? min(sr.past + (int)(row / G), g.cap - 1) : hi_lim;
+        for (int rt = 0; rt < RT; ++rt) {                  // rows that do not exist count as the last
+            const int row = row0 + 16 * rt + l16;
+            lim[rt] = row < n_rows ? min(sr.past + row / G, g.cap - 1) : hi_lim;
         }
-        const int stride = SPLIT ? 4 : 1, first = b0 + (SPLIT ? wave : 0), end = min(b1, (hi_lim >> 5) + 1);
-
-        float m[RT], nm[RT], l[RT];
-        f32x4 o[RT][S::NT];
-        int E = EMIN;
-        float Rmax = pow2i(EMIN), rinv = pow2i(-EMIN);     // 2^E, 2^-E
+    }
+    __device__ inline void start() {
+        E = EMIN;
+        Rmax = pow2i(EMIN);
+        rinv = pow2i(-EMIN);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             m[rt] = -__builtin_inff();
             nm[rt] = 0.f;
             l[rt] = 0.f;
 #pragma unroll
-            for (int t = 0; t < S::NT; ++t) o[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < L::NT; ++t) o[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        auto compute = [&](const Raw<DH, BITS> &r, int blk) {
-            if (!r.in) return;
-            const int key0 = blk * 32 + 8 * grp;           // this lane's eight keys
-            const bool edge = blk * 32 + 31 > lo_lim;
-            f32x4 st[RT][2];
+    }
+    // S^T of a block, kop(t, ks) the key operands
+    template <typename F>
+    __device__ inline void scores(f32x4 (&st)[RT][2], F &&kop) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const f16x2 z1 = both(g.k_zero ? r.kz[t] : QMID);
-                const f16x2 z[4] = {z1, z1, z1, z1};
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) st[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int rt = 0; rt < RT; ++rt) st[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < S::KS; ++ks) {
-                    uint32_t w0, w1;
-                    if constexpr (BITS == 8) {
-                        w0 = r.k[t][2 * ks];
-                        w1 = r.k[t][2 * ks + 1];
-                    } else if constexpr (DH >= 64) {       // the first half of the steps: low nibbles
-                        const int c = 2 * (ks % (S::KS / 2)), sft = ks < S::KS / 2 ? 0 : 4;
-                        w0 = (r.k[t][c] >> sft) & 0x0F0F0F0Fu;
-                        w1 = (r.k[t][c + 1] >> sft) & 0x0F0F0F0Fu;
-                    } else {
-                        const int sft = (grp & 1) * 4;
-                        w0 = (r.k[t][0] >> sft) & 0x0F0F0F0Fu;
-                        w1 = (r.k[t][1] >> sft) & 0x0F0F0F0Fu;
-                    }
-                    const f16x8 a = codes8(w0, w1, z);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int p = 0; p < S::NP; ++p) st[rt][t] = mma16(a, qf[rt][p][ks], st[rt][t]);
-                }
-            }
-            float vs[8], big = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                vs[i] = r.vs[i >> 2][i & 3];
-                if (edge) vs[i] = key0 + i <= hi_lim ? vs[i] : 0.f;             // what was never written may be anything
-                big = fmaxf(big, fabsf(vs[i]));
-            }
-            float top[RT];
-            bool move = big > Rmax;
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                top[rt] = -__builtin_inff();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float t = st[rt][i >> 2][i & 3] * r.ks[i >> 2][i & 3];
-                    if (edge) t = key0 + i <= lim[rt] ? t : -__builtin_inff();
-                    st[rt][i >> 2][i & 3] = t;
-                    top[rt] = fmaxf(top[rt], t);
-                }
-                move |= top[rt] * fs[rt] > m[rt] + LAZY;
-            }
-            if (__builtin_amdgcn_ballot_w64(move)) {       // the references move, with every sum so far
-                big = fmaxf(big, __shfl_xor(big, 16, 64));
-                big = fmaxf(big, __shfl_xor(big, 32, 64));
-                int En = E;
-                if (big > Rmax) En = min((int)(__builtin_bit_cast(uint32_t, big) >> 23) - 127 + 1, 125);
-                En = __builtin_amdgcn_readfirstlane(En);
-                const float down = pow2i(max(E - En, -126));
-                E = En;
-                Rmax = pow2i(E);
-                rinv = pow2i(-E);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    float t = top[rt];
-                    t = fmaxf(t, __shfl_xor(t, 16, 64));
-                    t = fmaxf(t, __shfl_xor(t, 32, 64));
-                    const float mn = fmaxf(m[rt], t * fs[rt]);
-                    const float al = mn == m[rt] ? 1.f : exp2f(m[rt] - mn);
-                    m[rt] = mn;
-                    nm[rt] = mn == -__builtin_inff() ? 0.f : -mn;
-                    l[rt] *= al;
-                    const float f = al * down;
-#pragma unroll
-                    for (int t2 = 0; t2 < S::NT; ++t2)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[rt][t2][i] *= f;
-                }
-            }
-            const float up = rinv * (float)(1 << WUP);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) vs[i] *= up;
-            f16x8 pw[RT][S::NP];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float w[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][i >> 2][i & 3], fs[rt], nm[rt]));
-                    l[rt] += p;
-                    w[i] = p * vs[i];
-                }
-#pragma unroll
-                for (int p = 0; p < S::NP; ++p)
-#pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
-                        const f16x2 hw = __builtin_convertvector(f32x2_t{w[i], w[i + 1]}, f16x2);
-                        pw[rt][p][i] = hw[0];
-                        pw[rt][p][i + 1] = hw[1];
-                        if (p + 1 < S::NP) {
-                            w[i] -= (float)hw[0];
-                            w[i + 1] -= (float)hw[1];
-                        }
-                    }
-            }
-            f16x2 z[4];
-            if (g.v_zero) {
-                z[0] = biased(r.vz[0], false);
-                z[1] = biased(r.vz[0], true);
-                z[2] = biased(r.vz[1], false);
-                z[3] = biased(r.vz[1], true);
-            } else {
-                z[0] = z[1] = z[2] = z[3] = both(QMID);
-            }
-#pragma unroll
-            for (int t = 0; t < S::NT; ++t) {
-                uint32_t w0, w1;
-                if constexpr (BITS == 8) {
-                    w0 = r.v[t][0];
-                    w1 = r.v[t][1];
-                } else if constexpr (DH >= 64) {
-                    const int c = t % (S::NT / 2), sft = t < S::NT / 2 ? 0 : 4;
-                    w0 = (r.v[c][0] >> sft) & 0x0F0F0F0Fu;
-                    w1 = (r.v[c][1] >> sft) & 0x0F0F0F0Fu;
-                } else {
-                    const int sft = (l16 >> 3) * 4;
-                    w0 = (r.v[0][0] >> sft) & 0x0F0F0F0Fu;
-                    w1 = (r.v[0][1] >> sft) & 0x0F0F0F0Fu;
-                }
-                const f16x8 a = codes8(w0, w1, z);
+            for (int ks = 0; ks < L::KS; ++ks) {
+                const f16x8 a = kop(t, ks);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                    for (int p = 0; p < S::NP; ++p) o[rt][t] = mma16(a, pw[rt][p], o[rt][t]);
-            }
-        };
-        if (first < end) {
-            Raw<DH, BITS> ra, rb;
-            int b = first;
-            load_block(g, s, h, b, lane, ra);
-            for (;;) {
-                if (b + stride < end) load_block(g, s, h, b + stride, lane, rb);
-                compute(ra, b);
-                b += stride;
-                if (b >= end) break;
-                if (b + stride < end) load_block(g, s, h, b + stride, lane, ra);
-                compute(rb, b);
-                b += stride;
-                if (b >= end) break;
+                    for (int p = 0; p < NP; ++p) st[rt][t] = mma16(a, qf[rt][p][ks], st[rt][t]);
+                if (ks & 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
-
-        // ---- sums over a row's four lane groups; the weights' scale taken back
+    }
+    // the scores in key units: times the keys' scales, -inf where not seen (key0: this lane's first key)
+    __device__ inline void scale(f32x4 (&st)[RT][2], const f32x4 (&ks)[2], bool edge, int key0) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) st[rt][i >> 2][i & 3] *= ks[i >> 2][i & 3];
+        if (edge) {
+            asm volatile("");                              // a branch, so that other blocks pay nothing for the masks
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    st[rt][i >> 2][i & 3] = key0 + i <= lim[rt] ? st[rt][i >> 2][i & 3] : -__builtin_inff();
+        }
+    }
+    // weights of a block's scores; moves the references where a score or a value scale asks for it
+    __device__ inline void weights(const f32x4 (&st)[RT][2], const f32x4 (&vsc)[2], bool edge, int key0, f16x8 (&pw)[RT][NP]) {
+        float vs[8], big = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) vs[i] = vsc[i >> 2][i & 3];
+        if (edge) {                                        // what was never written may be anything
+            asm volatile("");
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vs[i] = key0 + i <= hi_lim ? vs[i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(vs[i]));
+        float top[RT];
+        bool move = big > Rmax;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            top[rt] = st[rt][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top[rt] = fmaxf(top[rt], st[rt][i >> 2][i & 3]);
+            move |= top[rt] * fs[rt] > m[rt] + LAZY;
+        }
+        if (__builtin_amdgcn_ballot_w64(move)) {
+            big = fmaxf(big, __shfl_xor(big, 16, 64));
+            big = fmaxf(big, __shfl_xor(big, 32, 64));
+            int En = E;
+            if (big > Rmax) En = min((int)(__builtin_bit_cast(uint32_t, big) >> 23) - 127 + 1, 125);
+            En = __builtin_amdgcn_readfirstlane(En);
+            const float down = pow2i(max(E - En, -126));
+            E = En;
+            Rmax = pow2i(E);
+            rinv = pow2i(-E);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                float t = top[rt];
+                t = fmaxf(t, __shfl_xor(t, 16, 64));
+                t = fmaxf(t, __shfl_xor(t, 32, 64));
+                const float mn = fmaxf(m[rt], t * fs[rt]);
+                const float al = mn == m[rt] ? 1.f : exp2f(m[rt] - mn);
+                m[rt] = mn;
+                nm[rt] = mn == -__builtin_inff() ? 0.f : -mn;
+                l[rt] *= al;
+                const float f = al * down;
+#pragma unroll
+                for (int t2 = 0; t2 < L::NT; ++t2)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[rt][t2][i] *= f;
+            }
+        }
+        const float up = rinv * (float)(1 << WUP);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) vs[i] *= up;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][i >> 2][i & 3], fs[rt], nm[rt]));
+                l[rt] += p;
+                w[i] = p * vs[i];
+            }
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const f16x2 hw = __builtin_convertvector(f32x2_t{w[i], w[i + 1]}, f16x2);
+                    pw[rt][p][i] = hw[0];
+                    pw[rt][p][i + 1] = hw[1];
+                    if (p + 1 < NP) {
+                        w[i] -= (float)hw[0];
+                        w[i + 1] -= (float)hw[1];
+                    }
+                }
+        }
+    }
+    // O^T += V^T P^T, vop(t) the value operands
+    template <typename F>
+    __device__ inline void values(const f16x8 (&pw)[RT][NP], F &&vop) {
+#pragma unroll
+        for (int t = 0; t < L::NT; ++t) {
+            const f16x8 a = vop(t);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) o[rt][t] = mma16(a, pw[rt][p], o[rt][t]);
+            if (t & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    // sums over a row's four lane groups; the weights' scale taken back
+    __device__ inline void finish() {
         const float back = pow2i(max(E - WUP, -126));
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             l[rt] += __shfl_xor(l[rt], 16, 64);
             l[rt] += __shfl_xor(l[rt], 32, 64);
 #pragma unroll
-            for (int t = 0; t < S::NT; ++t)
+            for (int t = 0; t < L::NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[rt][t][i] *= back;
         }
-        // one row's four elements d .. d + 3: the output, or the split's share of it
-        auto put = [&](int64_t row, int d, f32x4 v, float mm, float ll) {
-            if (row >= n_rows) return;
-            const int64_t tok = sr.row + row / G, head = (int64_t)h * G + row % G;
-            if (n_split == 1) {
-                const float inv = ll == 0.f ? 0.f : 1.f / ll;
-                store4<DT>(static_cast<elem *>(av) + (tok * g.n_heads + head) * DH + d,
-                           f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
-            } else {
-                float *pp = part + ((tok * g.n_heads + head) * n_split + split) * (DH + 4);
-                *reinterpret_cast<f32x4 *>(pp + d) = v;
-                if (d == 0) {
-                    pp[DH] = mm;
-                    pp[DH + 1] = ll;
+    }
+};
+
+// Queries in LDS: QP fp16 per row (padding against bank conflicts), the parts `stride` apart
+template <int DH> constexpr int QP = DH < 32 ? 40 : DH + 8;
+
+// One query row by one wave: turned, scaled by a power of two, as fp16 parts into row `slot` of ql; returns the
+// score scale in exp2 units with the power of two taken back (NaN for a row that is not finite)
+template <int DT, int DH, int NP>
+__device__ inline float query_row(const CacheArgs &g, const SeqRows &sr, const void *yv, int64_t ldy, int h, int G, int row,
+                                  int n_rows, _Float16 *ql, int slot, int stride, int lane) {
+    typedef typename Mma<DT>::elem elem;
+    constexpr int HALF = DH / 2;
+    float x0 = 0.f, x1 = 0.f;
+    const bool live = lane < HALF && row < n_rows;
+    const int i = live ? row / G : 0;
+    if (live) {
+        const elem *q = static_cast<const elem *>(yv) + (int64_t)(sr.row + i) * ldy + ((int64_t)h * G + row % G) * DH + lane;
+        x0 = to_f32<DT>(q[0]);
+        x1 = to_f32<DT>(q[HALF]);
+    }
+    uint32_t mx = max(__builtin_bit_cast(uint32_t, x0) & 0x7FFFFFFFu, __builtin_bit_cast(uint32_t, x1) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, off, 64));
+    const int e = min(max((int)(mx >> 23) - 127, -100), 127);                   // exponent of the largest element
+    const float up = pow2i(max(3 - e, -126));
+    x0 *= up;
+    x1 *= up;
+    if (g.freq[0] != 0.0 && live) {
+        // whole cycles are taken off the angle in fp64, the rest is fp32
+        const double cyc = (double)(sr.past + i) * g.freq[lane] * 0.15915494309189535;
+        float sn, cs;
+        sincospif((float)(2.0 * (cyc - rint(cyc))), &sn, &cs);
+        const float a = x0, b = x1;
+        x0 = a * cs - b * sn;
+        x1 = b * cs + a * sn;
+    }
+    const bool fine = mx < 0x7F800000u;
+    if (lane < HALF) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const _Float16 a = fine ? (_Float16)x0 : (_Float16)0.f, b = fine ? (_Float16)x1 : (_Float16)0.f;
+            ql[p * stride + slot * QP<DH> + lane] = a;
+            ql[p * stride + slot * QP<DH> + lane + HALF] = b;
+            x0 -= (float)a;
+            x1 -= (float)b;
+        }
+    }
+    if constexpr (DH < 32)
+        if (lane >= DH && lane < 32)
+            for (int p = 0; p < NP; ++p) ql[p * stride + slot * QP<DH> + lane] = (_Float16)0.f;
+    return fine ? LOG2E / sqrtf((float)DH) / up : __builtin_nanf("");
+}
+
+template <int DT>
+__device__ inline void store4(typename Mma<DT>::elem *p, f32x4 v) {
+    if constexpr (DT == F32) *reinterpret_cast<f32x4 *>(p) = v;
+    else *reinterpret_cast<u32x2 *>(p) = u32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+}
+// four elements d .. d + 3 of a row: the output, or the split's share of it (O, m, l)
+template <int DT, int DH>
+__device__ inline void put_row(const CacheArgs &g, const SeqRows &sr, int h, int G, int row, int d, f32x4 v, float m, float l,
+                               void *av, float *part, int split, int n_split) {
+    typedef typename Mma<DT>::elem elem;
+    const int64_t at = (int64_t)(sr.row + row / G) * g.n_heads + (int64_t)h * G + row % G;
+    if (n_split == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        store4<DT>(static_cast<elem *>(av) + at * DH + d, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
+    } else {
+        float *pp = part + (at * n_split + split) * (DH + 4);
+        *reinterpret_cast<f32x4 *>(pp + d) = v;
+        if (d == 0) {
+            pp[DH] = m;
+            pp[DH + 1] = l;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- few rows
+// The four waves of a workgroup share 16 RT rows and deal out the key blocks.  Codes go from memory to
+// registers; a block's keys are asked for once the previous block's scores are formed, its values once the
+// previous block's are used, so one block is in flight per wave without a second set of registers.
+template <int DT, int DH, int BITS, int RT>
+struct FewCfg {
+    static constexpr size_t Q_LDS = (size_t)Wave<DT, DH, BITS, RT>::NP * 16 * RT * QP<DH> * 2;
+    static constexpr size_t O_LDS = (size_t)4 * 16 * RT * (DH + 4) * 4;
+    static constexpr size_t LDS = Q_LDS > O_LDS ? Q_LDS : O_LDS;
+};
+
+// grid: x = (sequence, key/value head, split), y = row tiles (dealt out)
+template <int DT, int DH, int BITS, int RT, int OCC>
+__global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy,
+                                                          void *__restrict__ av, float *__restrict__ part, int n_split) {
+    typedef Wave<DT, DH, BITS, RT> W;
+    typedef Lay<DH, BITS> L;
+    constexpr int QMID = (1 << (BITS - 1)) - 1, ROWS = 16 * RT;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float rowf[ROWS];
+    __shared__ float ml[4][ROWS][2];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int l16 = lane & 15, grp = lane >> 4;
+    const int split = blockIdx.x % n_split, sh = blockIdx.x / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
+    const SeqRows sr = seq_rows(g, s);
+    const int G = g.n_heads / g.n_kv_heads;
+    const int n_rows = sr.n * G;
+    const int len = (int)min((int64_t)sr.past + sr.n, (int64_t)g.cap), n_blk = (len + 31) >> 5;
+    const int b0 = (int)((int64_t)n_blk * split / n_split), b1 = (int)((int64_t)n_blk * (split + 1) / n_split);
+    const bool asym = g.k_zero != nullptr;
+
+    for (int tile = blockIdx.y, row0; (row0 = tile * ROWS) < n_rows; tile += gridDim.y) {
+        W w;
+        _Float16 *ql = reinterpret_cast<_Float16 *>(smem);
+        __syncthreads();                                   // LDS of the tile before
+#pragma unroll 1
+        for (int r = wave; r < ROWS; r += 4) {
+            const float f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + r, n_rows, ql, r, ROWS * QP<DH>, lane);
+            if (lane == 0) rowf[r] = f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            w.fs[rt] = rowf[16 * rt + l16];
+#pragma unroll
+            for (int p = 0; p < W::NP; ++p)
+#pragma unroll
+                for (int ks = 0; ks < L::KS; ++ks)
+                    w.qf[rt][p][ks] = *reinterpret_cast<const f16x8 *>(ql + p * ROWS * QP<DH> + (16 * rt + l16) * QP<DH> + L::dim(ks, grp));
+        }
+        w.limits(g, sr, G, row0, n_rows, l16);
+        w.start();
+        const int end = min(b1, (w.hi_lim >> 5) + 1);
+
+        u32x2 k[2][L::KU], v[L::VU], vz = {0, 0};
+        f32x4 ks[2], vs[2];
+        int kz[2] = {QMID, QMID};
+        // a lane's byte offsets inside a block; its first slot is wave-uniform
+        const uint32_t zoff = L::key(0, l16), koff = zoff * L::DHB + L::kbyte(0, grp), voff = L::vrow(0, l16) * 32 + 8 * grp;
+        auto load_k = [&](int64_t slot) {
+            const uint8_t *kb = g.k + slot * L::DHB, *sb = reinterpret_cast<const uint8_t *>(g.k_scale + slot);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int u = 0; u < L::KU; u += 2) {
+                    if constexpr (L::KU >= 2) {            // two units are 16 bytes
+                        const u32x4 q = ldu<u32x4>(kb, koff + 4 * t * L::DHB + 64 * (u >> 1));
+                        k[t][u] = u32x2{q[0], q[1]};
+                        k[t][u + 1] = u32x2{q[2], q[3]};
+                    } else {
+                        k[t][0] = ldu<u32x2>(kb, koff + 4 * t * L::DHB);
+                    }
                 }
+                if (asym) kz[t] = ldu<uint8_t>(g.k_zero + slot, zoff + 4 * t);
+                ks[t] = ldu<f32x4>(sb, 32 * grp + 16 * t);
             }
         };
-        if constexpr (!SPLIT) {
+        auto load_v = [&](int64_t slot) {
+            const uint8_t *vb = g.v + slot * L::DHB, *sb = reinterpret_cast<const uint8_t *>(g.v_scale + slot);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int u = 0; u < L::VU; ++u) v[u] = ldu<u32x2>(vb, voff + 512 * u);
 #pragma unroll
-                for (int t = 0; t < S::NT; ++t) put(row0 + 16 * rt + l16, 16 * t + 4 * grp, o[rt][t], m[rt], l[rt]);
-        } else {
-            // the four waves' sums, through LDS
-            float *ol = reinterpret_cast<float *>(smem);
-            __syncthreads();                               // every wave has its queries
+            for (int t = 0; t < 2; ++t) vs[t] = ldu<f32x4>(sb, 32 * grp + 16 * t);
+            if (asym) vz = ldu<u32x2>(g.v_zero + slot, 8 * grp);
+        };
+        // blocks wave, wave + 4, ... of the split; a block without a page loads page 0 and is not used
+        int b = b0 + wave;
+        if (b < end) {
+            int64_t slot = block_slot(g, s, h, b);
+            load_k(max(slot, (int64_t)0));
+            load_v(max(slot, (int64_t)0));
+            for (;;) {
+                const bool more = b + 4 < end;
+                const int64_t next = more ? block_slot(g, s, h, b + 4) : -1;
+                // no page: nothing of the block is seen
+                const int key0 = slot >= 0 ? b * 32 + 8 * grp : NOWHERE;
+                const bool edge = slot < 0 || b * 32 + 31 > w.lo_lim;
+                f32x4 st[RT][2];
+                f16x8 pw[RT][W::NP];
+                f16x2 zk[2][4];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                if (grp == 0) {
-                    mlE[wave][16 * rt + l16][0] = m[rt];
-                    mlE[wave][16 * rt + l16][1] = l[rt];
-                }
+                for (int t = 0; t < 2; ++t) zk[t][0] = zk[t][1] = zk[t][2] = zk[t][3] = both(kz[t]);
+                w.scores(st, [&](int t, int step) { return L::kop(k[t], step, grp, zk[t]); });
+                w.scale(st, ks, edge, key0);
+                __builtin_amdgcn_sched_barrier(0);
+                load_k(max(next, (int64_t)0));             // after the last block: page 0, not used
+                __builtin_amdgcn_sched_barrier(0);
+                w.weights(st, vs, edge, key0, pw);
+                f16x2 zv[4] = {biased(vz[0], false), biased(vz[0], true), biased(vz[1], false), biased(vz[1], true)};
+                if (!asym) zv[0] = zv[1] = zv[2] = zv[3] = both(QMID);
+                w.values(pw, [&](int t) { return L::vop(v, t, l16, zv); });
+                __builtin_amdgcn_sched_barrier(0);
+                if (!more) break;
+                load_v(max(next, (int64_t)0));
+                __builtin_amdgcn_sched_barrier(0);
+                slot = next;
+                b += 4;
+            }
+        }
+        w.finish();
+
+        // ---- the four waves' sums, through LDS
+        float *ol = reinterpret_cast<float *>(smem);
+        __syncthreads();                                   // every wave has its queries
 #pragma unroll
-                for (int t = 0; t < S::NT; ++t)
-                    *reinterpret_cast<f32x4 *>(ol + ((wave * 16 * RT) + 16 * rt + l16) * (DH + 4) + 16 * t + 4 * grp) = o[rt][t];
+        for (int rt = 0; rt < RT; ++rt) {
+            if (grp == 0) {
+                ml[wave][16 * rt + l16][0] = w.m[rt];
+                ml[wave][16 * rt + l16][1] = w.l[rt];
+            }
+#pragma unroll
+            for (int t = 0; t < L::NT; ++t)
+                *reinterpret_cast<f32x4 *>(ol + (wave * ROWS + 16 * rt + l16) * (DH + 4) + 16 * t + 4 * grp) = w.o[rt][t];
+        }
+        __syncthreads();
+        const int live = min(ROWS, n_rows - row0);
+        for (int c = threadIdx.x; c < live * (DH / 4); c += 256) {
+            const int r = c / (DH / 4), d = c % (DH / 4) * 4;
+            float mm = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mm = fmaxf(mm, ml[i][r][0]);
+            f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+            float ll = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // a wave without a key has m = -inf, l = 0; a NaN row keeps m = -inf and l = NaN
+                const float f = ml[i][r][0] == mm ? 1.f : exp2f(ml[i][r][0] - mm);
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(ol + (i * ROWS + r) * (DH + 4) + d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += f * x[e];
+                ll += f * ml[i][r][1];
+            }
+            put_row<DT, DH>(g, sr, h, G, row0 + r, d, sum, mm, ll, av, part, split, n_split);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- many rows
+// Each wave has 32 rows of its own; the workgroup turns two blocks of 32 tokens at a time into operands in LDS,
+// which its four waves share (waves 0, 1 the keys, 2, 3 the values of the two blocks; an operand is 64 lanes x 16
+// bytes, written and read without conflicts).  The next two blocks' bytes are in flight meanwhile; two stages, one
+// barrier per stage.
+template <int DT, int DH, int BITS>
+struct ManyCfg {
+    typedef Lay<DH, BITS> L;
+    static constexpr int RT = 2, ROWS = 128;
+    static constexpr int KOPS = 2 * L::KS, OPS = KOPS + L::NT;                   // operands of a block
+    static constexpr int BLOCK = OPS * 1024 + 256;                               // and its 32 + 32 scales
+    static constexpr size_t STAGE = 2 * BLOCK;
+    static constexpr size_t Q_LDS = (size_t)Wave<DT, DH, BITS, RT>::NP * 4 * 16 * QP<DH> * 2;
+    static constexpr size_t LDS = 2 * STAGE > Q_LDS ? 2 * STAGE : Q_LDS;
+};
+
+template <int DT, int DH, int BITS>
+__global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy,
+                                                           void *__restrict__ av, float *__restrict__ part, int n_split) {
+    typedef ManyCfg<DT, DH, BITS> S;
+    typedef Wave<DT, DH, BITS, S::RT> W;
+    typedef Lay<DH, BITS> L;
+    constexpr int QMID = (1 << (BITS - 1)) - 1, RT = S::RT;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float rowf[64];
+    __shared__ int has[2][2];                              // per stage and block: its page exists
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int l16 = lane & 15, grp = lane >> 4;
+    const int split = blockIdx.x % n_split, sh = blockIdx.x / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
+    const SeqRows sr = seq_rows(g, s);
+    const int G = g.n_heads / g.n_kv_heads;
+    const int n_rows = sr.n * G, n_tiles = (n_rows + S::ROWS - 1) / S::ROWS;
+    const int len = (int)min((int64_t)sr.past + sr.n, (int64_t)g.cap), n_blk = (len + 31) >> 5;
+    const int b0 = (int)((int64_t)n_blk * split / n_split), b1 = (int)((int64_t)n_blk * (split + 1) / n_split);
+    const bool asym = g.k_zero != nullptr;
+    const int kind = wave >> 1, mine = wave & 1;           // what this wave prepares: keys or values, of which block
+
+    // the last tiles see the most keys: first
+    for (int tile = n_tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= gridDim.y) {
+        const int row0 = tile * S::ROWS + wave * 16 * RT;
+        W w;
+        _Float16 *ql = reinterpret_cast<_Float16 *>(smem) + wave * 16 * QP<DH>;
+        constexpr int QSTRIDE = 4 * 16 * QP<DH>;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            __syncthreads();                               // LDS of the tile before, and of the rows before
+#pragma unroll 1
+            for (int r = 0; r < 16; ++r) {
+                const float f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + 16 * rt + r, n_rows, ql, r, QSTRIDE, lane);
+                if (lane == 0) rowf[wave * 16 + r] = f;
             }
             __syncthreads();
-            const int live = (int)min((int64_t)16 * RT, n_rows - row0);
-            for (int c = threadIdx.x; c < live * (DH / 4); c += 256) {
-                const int r = c / (DH / 4), d = c % (DH / 4) * 4;
-                float mm = -__builtin_inff();
+            w.fs[rt] = rowf[wave * 16 + l16];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) mm = fmaxf(mm, mlE[w][r][0]);
-                f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-                float ll = 0.f;
+            for (int p = 0; p < W::NP; ++p)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    // a wave without a key has m = -inf, l = 0; a NaN row keeps m = -inf and l = NaN
-                    const float f = mlE[w][r][0] == mm ? 1.f : exp2f(mlE[w][r][0] - mm);
-                    const f32x4 x = *reinterpret_cast<const f32x4 *>(ol + (w * 16 * RT + r) * (DH + 4) + d);
+                for (int ks = 0; ks < L::KS; ++ks)
+                    w.qf[rt][p][ks] = *reinterpret_cast<const f16x8 *>(ql + p * QSTRIDE + l16 * QP<DH> + L::dim(ks, grp));
+        }
+        __syncthreads();                                   // the stages lie over the queries
+        w.limits(g, sr, G, row0, n_rows, l16);
+        w.start();
+        const int last = min((tile + 1) * S::ROWS, n_rows) - 1;
+        const int end = min(b1, (min(sr.past + last / G, g.cap - 1) >> 5) + 1);   // of the workgroup's rows
+
+        u32x2 raw[2 * L::KU > L::VU ? 2 * L::KU : L::VU], vz = {0, 0};
+        int kz[2] = {QMID, QMID};
+        float sc = 0.f;
+        int64_t slot = -1;
+        const uint32_t zoff = L::key(0, l16), koff = zoff * L::DHB + L::kbyte(0, grp), voff = L::vrow(0, l16) * 32 + 8 * grp;
+        auto load = [&](int b) {                           // this wave's share of blocks b, b + 1
+            slot = b + mine < end ? block_slot(g, s, h, b + mine) : -1;
+            const int64_t at = max(slot, (int64_t)0);
+            if (kind == 0) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] += f * x[i];
-                    ll += f * mlE[w][r][1];
+                for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                    for (int u = 0; u < L::KU; ++u)
+                        raw[t * L::KU + u] = ldu<u32x2>(g.k + at * L::DHB, koff + 4 * t * L::DHB + L::kbyte(u, 0));
+                    if (asym) kz[t] = ldu<uint8_t>(g.k_zero + at, zoff + 4 * t);
                 }
-                put(row0 + r, d, v, mm, ll);
+                sc = ldu<float>(reinterpret_cast<const uint8_t *>(g.k_scale + at), 4 * (lane & 31));
+            } else {
+#pragma unroll
+                for (int u = 0; u < L::VU; ++u) raw[u] = ldu<u32x2>(g.v + at * L::DHB, voff + 512 * u);
+                if (asym) vz = ldu<u32x2>(g.v_zero + at, 8 * grp);
+                sc = ldu<float>(reinterpret_cast<const uint8_t *>(g.v_scale + at), 4 * (lane & 31));
             }
+        };
+        auto prepare = [&](int buf) {                      // into stage buf
+            unsigned char *blk = smem + buf * S::STAGE + mine * S::BLOCK;
+            if (kind == 0) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const f16x2 z1 = both(kz[t]), z[4] = {z1, z1, z1, z1};
+                    u32x2 k[L::KU];
+#pragma unroll
+                    for (int u = 0; u < L::KU; ++u) k[u] = raw[t * L::KU + u];
+#pragma unroll
+                    for (int ks = 0; ks < L::KS; ++ks)
+                        *reinterpret_cast<f16x8 *>(blk + (t * L::KS + ks) * 1024 + lane * 16) = L::kop(k, ks, grp, z);
+                }
+                if (lane == 0) has[buf][mine] = slot >= 0;
+            } else {
+                f16x2 z[4] = {biased(vz[0], false), biased(vz[0], true), biased(vz[1], false), biased(vz[1], true)};
+                if (!asym) z[0] = z[1] = z[2] = z[3] = both(QMID);
+                u32x2 v[L::VU];
+#pragma unroll
+                for (int u = 0; u < L::VU; ++u) v[u] = raw[u];
+#pragma unroll
+                for (int t = 0; t < L::NT; ++t)
+                    *reinterpret_cast<f16x8 *>(blk + (S::KOPS + t) * 1024 + lane * 16) = L::vop(v, t, l16, z);
+            }
+            if (lane < 32) *reinterpret_cast<float *>(blk + S::OPS * 1024 + kind * 128 + lane * 4) = sc;
+        };
+        int buf = 0;
+        if (b0 < end) load(b0);
+        for (int b = b0; b < end; b += 2) {
+            prepare(buf);
+            if (b + 2 < end) load(b + 2);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const unsigned char *blk = smem + buf * S::STAGE + i * S::BLOCK;
+                if ((b + i) * 32 > w.hi_lim || b + i >= end || !__builtin_amdgcn_readfirstlane(has[buf][i])) continue;
+                const int key0 = (b + i) * 32 + 8 * grp;
+                const bool edge = (b + i) * 32 + 31 > w.lo_lim;
+                const f32x4 *scl = reinterpret_cast<const f32x4 *>(blk + S::OPS * 1024);
+                f32x4 st[RT][2];
+                f16x8 pw[RT][W::NP];
+                w.scores(st, [&](int t, int ks) { return *reinterpret_cast<const f16x8 *>(blk + (t * L::KS + ks) * 1024 + lane * 16); });
+                const f32x4 ks[2] = {scl[2 * grp], scl[2 * grp + 1]}, vs[2] = {scl[8 + 2 * grp], scl[8 + 2 * grp + 1]};
+                w.scale(st, ks, edge, key0);
+                w.weights(st, vs, edge, key0, pw);
+                w.values(pw, [&](int t) { return *reinterpret_cast<const f16x8 *>(blk + (S::KOPS + t) * 1024 + lane * 16); });
+            }
+            buf ^= 1;
+        }
+        w.finish();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = row0 + 16 * rt + l16;
+            if (row < n_rows)
+#pragma unroll
+                for (int t = 0; t < L::NT; ++t)
+                    put_row<DT, DH>(g, sr, h, G, row, 16 * t + 4 * grp, w.o[rt][t], w.m[rt], w.l[rt], av, part, split, n_split);
         }
     }
 }
@@ -545,14 +733,13 @@ Plan plan_of(const CacheArgs &g) {
     return p;
 }
 
-template <int DT, int DH, int BITS, int RT, bool SPLIT>
-hipError_t run_attn(const CacheArgs &g, const Plan &p, const void *y, int64_t ldy, void *a, float *part, hipStream_t st) {
-    typedef AttnCfg<DT, DH, BITS, RT, SPLIT> S;
-    hipError_t e = hipFuncSetAttribute((const void *)attn_cache_kernel<DT, DH, BITS, RT, SPLIT>,
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::LDS);
+template <int DT, int DH, typename K>
+hipError_t run_attn(K kernel, size_t lds, const CacheArgs &g, const Plan &p, const void *y, int64_t ldy, void *a, float *part,
+                    hipStream_t st) {
+    hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)(g.n_seq * g.n_kv_heads * p.n_split), (unsigned)std::min<int64_t>(p.tiles, 65535));
-    attn_cache_kernel<DT, DH, BITS, RT, SPLIT><<<grid, 256, S::LDS, st>>>(g, y, ldy, a, part, p.n_split);
+    kernel<<<grid, 256, lds, st>>>(g, y, ldy, a, part, p.n_split);
     e = hipGetLastError();
     if (e != hipSuccess || p.n_split == 1) return e;
     const int64_t items = (int64_t)std::max(g.max_new, 1) * g.n_heads;
@@ -564,9 +751,11 @@ template <int DT, int DH, int BITS>
 hipError_t run_plan(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
     const Plan p = plan_of(g);
     float *part = static_cast<float *>(ws);
-    if (!p.split_waves) return run_attn<DT, DH, BITS, 2, false>(g, p, y, ldy, a, part, st);
-    return p.rt == 1 ? run_attn<DT, DH, BITS, 1, true>(g, p, y, ldy, a, part, st)
-                     : run_attn<DT, DH, BITS, 2, true>(g, p, y, ldy, a, part, st);
+    if (!p.split_waves)
+        return run_attn<DT, DH>(attn_many_kernel<DT, DH, BITS>, ManyCfg<DT, DH, BITS>::LDS, g, p, y, ldy, a, part, st);
+    constexpr int OCC1 = DT == BF16 ? 3 : 2, OCC2 = 1;
+    return p.rt == 1 ? run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 1, OCC1>, FewCfg<DT, DH, BITS, 1>::LDS, g, p, y, ldy, a, part, st)
+                     : run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 2, OCC2>, FewCfg<DT, DH, BITS, 2>::LDS, g, p, y, ldy, a, part, st);
 }
 template <int DT, int DH>
 hipError_t run_bits(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
