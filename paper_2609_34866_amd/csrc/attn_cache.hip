@@ -667,44 +667,85 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
     }
 }
 
-// The splits of a row joined: one wave per (token, head) and pass, the splits over its lane groups.
-// part [row][split][DH + 4]: O, m, l
-template <int DT, int DH>
+// The splits of a row joined; part [row][split][DH + 4]: O, m, l.  LANES threads per (token, head): a wave where
+// there are few splits (and then many rows), else a workgroup, so that all of a row's loads are in flight at once.
+constexpr int MOST_SPLITS = 128;
+template <int DT, int DH, int LANES>
 __global__ __launch_bounds__(256) void attn_join_kernel(CacheArgs g, const float *__restrict__ part, void *__restrict__ av,
                                                         int n_split) {
     typedef typename Mma<DT>::elem elem;
-    constexpr int LPR = DH / 4, SG = 64 / LPR;             // lanes of a row, splits at once
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    constexpr int LPR = DH / 4, SG = LANES / LPR, RPB = 256 / LANES;             // lanes of a row's elements, splits at once
+    constexpr int WS = LANES / 64;                                               // waves of a row
+    __shared__ float fac[RPB][MOST_SPLITS];
+    __shared__ float2 ml[RPB][WS];
+    __shared__ f32x4 sum[WS][LPR];
+    const int tid = threadIdx.x % LANES, lane = threadIdx.x & 63;
+    const int r = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / LANES)), wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int s = blockIdx.x;
     const SeqRows sr = seq_rows(g, s);
     const int64_t items = (int64_t)sr.n * g.n_heads;
-    const int d = lane % LPR * 4, sg = lane / LPR;
-    for (int64_t it = (int64_t)blockIdx.y * 4 + wave; it < items; it += (int64_t)gridDim.y * 4) {
-        const int64_t row = (int64_t)sr.row * g.n_heads + it;
+    const int d = tid % LPR * 4, sg = tid / LPR;
+    for (int64_t it0 = (int64_t)blockIdx.y * RPB; it0 < items; it0 += (int64_t)gridDim.y * RPB) {
+        const int64_t it = min(it0 + r, items - 1), row = (int64_t)sr.row * g.n_heads + it;     // (the last row twice: same values)
         const float *p = part + row * n_split * (DH + 4);
-        float m = -__builtin_inff();
-        for (int i = lane; i < n_split; i += 64) m = fmaxf(m, p[(int64_t)i * (DH + 4) + DH]);
+        // thread i the factor of split i (two for a wave of 64)
+        float mi[(MOST_SPLITS + LANES - 1) / LANES], li[(MOST_SPLITS + LANES - 1) / LANES], m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+        for (int k = 0; k < (MOST_SPLITS + LANES - 1) / LANES; ++k) {
+            const int i = tid + k * LANES;
+            mi[k] = i < n_split ? p[(int64_t)i * (DH + 4) + DH] : -__builtin_inff();
+            li[k] = i < n_split ? p[(int64_t)i * (DH + 4) + DH + 1] : 0.f;
+            m = fmaxf(m, mi[k]);
+        }
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+        if constexpr (WS > 1) {
+            __syncthreads();                               // the row before is done with ml, fac and sum
+            if (lane == 0) ml[r][wv].x = m;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WS; ++w) m = fmaxf(m, ml[r][w].x);
+        }
+#pragma unroll
+        for (int k = 0; k < (MOST_SPLITS + LANES - 1) / LANES; ++k) {
+            const int i = tid + k * LANES;
+            const float f = mi[k] == m ? 1.f : exp2f(mi[k] - m);
+            if (i < n_split) fac[r][i] = f;
+            l += f * li[k];
+        }
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);
+        if (WS > 1 && lane == 0) ml[r][wv].y = l;
+        __syncthreads();
+        if constexpr (WS > 1) {
+            l = 0.f;
+#pragma unroll
+            for (int w = 0; w < WS; ++w) l += ml[r][w].y;
+        }
         f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-        float l = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int i = sg; i < n_split; i += SG) {
-            const float *q = p + (int64_t)i * (DH + 4);
-            const float mi = q[DH], f = mi == m ? 1.f : exp2f(mi - m);
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(q + d);
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(p + (int64_t)i * (DH + 4) + d);
+            const float f = fac[r][i];
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] += f * x[k];
-            l += f * q[DH + 1];
         }
 #pragma unroll
-        for (int off = 32; off >= LPR; off >>= 1) {
+        for (int off = 32; off >= LPR; off >>= 1)
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] += __shfl_xor(v[k], off, 64);
-            l += __shfl_xor(l, off, 64);
+        if constexpr (WS > 1) {
+            if (lane < LPR) sum[wv][lane] = v;
+            __syncthreads();
+            if (tid < LPR) {
+                v = sum[0][tid];
+#pragma unroll
+                for (int w = 1; w < WS; ++w)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] += sum[w][tid][k];
+            }
         }
-        if (sg == 0) {
+        if (tid < LPR) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
             store4<DT>(static_cast<elem *>(av) + row * DH + d, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
         }
@@ -729,7 +770,7 @@ Plan plan_of(const CacheArgs &g) {
     // enough workgroups for every CU to hold several, each with at least 8 blocks of 32 keys
     const int64_t base = (int64_t)g.n_seq * g.n_kv_heads * p.tiles, blocks = ((int64_t)g.cap + 31) / 32;
     const int64_t want = (4 * CUS + base - 1) / base, most = std::max<int64_t>(1, blocks / 8);
-    p.n_split = (int)std::min<int64_t>(std::min(want, most), 128);
+    p.n_split = (int)std::min<int64_t>(std::min(want, most), MOST_SPLITS);
     return p;
 }
 
@@ -743,7 +784,9 @@ hipError_t run_attn(K kernel, size_t lds, const CacheArgs &g, const Plan &p, con
     e = hipGetLastError();
     if (e != hipSuccess || p.n_split == 1) return e;
     const int64_t items = (int64_t)std::max(g.max_new, 1) * g.n_heads;
-    attn_join_kernel<DT, DH><<<dim3(g.n_seq, (unsigned)std::min<int64_t>((items + 3) / 4, 65535)), 256, 0, st>>>(g, part, a, p.n_split);
+    const auto join = p.n_split <= 8 ? attn_join_kernel<DT, DH, 64> : attn_join_kernel<DT, DH, 256>;
+    const int64_t rows = p.n_split <= 8 ? 4 : 1;
+    join<<<dim3(g.n_seq, (unsigned)std::min<int64_t>((items + rows - 1) / rows, 65535)), 256, 0, st>>>(g, part, a, p.n_split);
     return hipGetLastError();
 }
 
