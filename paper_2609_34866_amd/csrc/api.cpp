@@ -1280,7 +1280,7 @@ jab_status jab_cache_read(const jab_problem *p, const jab_cache *c, const jab_ca
 
 size_t jab_attn_cache_workspace(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r) {
     if (check_cache_sizes(p, c, r) != JAB_OK) return (size_t)-1;
-    return jab::attn_cache_ws_bytes(cache_args(*p, *c, *r));
+    return jab::attn_cache_ws_bytes(p->dtype, cache_args(*p, *c, *r));
 }
 
 jab_status jab_attn_cache(const jab_problem *p, const jab_cache *c, const jab_cache_rows *r, const void *y, void *a, void *ws,
@@ -1290,7 +1290,7 @@ jab_status jab_attn_cache(const jab_problem *p, const jab_cache *c, const jab_ca
     JAB_CHECK(y && aligned(y, 16) && a && aligned(a, 16), JAB_E_INVALID, "y / a NULL or not 16-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(stream);
     const jab::CacheArgs g = cache_args(*p, *c, *r);
-    const size_t need = jab::attn_cache_ws_bytes(g);
+    const size_t need = jab::attn_cache_ws_bytes(p->dtype, g);
     if (need) {
         JAB_CHECK(ws && aligned(ws, 256), JAB_E_INVALID, "workspace is NULL or not 256-byte aligned");
         JAB_CHECK(ws_bytes >= need, JAB_E_WORKSPACE, "workspace too small for jab_attn_cache");

@@ -392,27 +392,8 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
 
     for (int tile = blockIdx.y, row0; (row0 = tile * ROWS) < n_rows; tile += gridDim.y) {
         W w;
-        _Float16 *ql = reinterpret_cast<_Float16 *>(smem);
-        __syncthreads();                                   // LDS of the tile before
-#pragma unroll 1
-        for (int r = wave; r < ROWS; r += 4) {
-            const float f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + r, n_rows, ql, r, ROWS * QP<DH>, lane);
-            if (lane == 0) rowf[r] = f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            w.fs[rt] = rowf[16 * rt + l16];
-#pragma unroll
-            for (int p = 0; p < W::NP; ++p)
-#pragma unroll
-                for (int ks = 0; ks < L::KS; ++ks)
-                    w.qf[rt][p][ks] = *reinterpret_cast<const f16x8 *>(ql + p * ROWS * QP<DH> + (16 * rt + l16) * QP<DH> + L::dim(ks, grp));
-        }
         w.limits(g, sr, G, row0, n_rows, l16);
-        w.start();
         const int end = min(b1, (w.hi_lim >> 5) + 1);
-
         u32x2 k[2][L::KU], v[L::VU], vz = {0, 0};
         f32x4 ks[2], vs[2];
         int kz[2] = {QMID, QMID};
@@ -444,12 +425,35 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
             for (int t = 0; t < 2; ++t) vs[t] = ldu<f32x4>(sb, 32 * grp + 16 * t);
             if (asym) vz = ldu<u32x2>(g.v_zero + slot, 8 * grp);
         };
-        // blocks wave, wave + 4, ... of the split; a block without a page loads page 0 and is not used
+        // blocks wave, wave + 4, ... of the split, the first one's bytes on their way before the queries are made; a
+        // block without a page, and past the end, loads page 0 and is not used
         int b = b0 + wave;
+        int64_t slot = b < end ? block_slot(g, s, h, b) : -1;
+        load_k(max(slot, (int64_t)0));
+        load_v(max(slot, (int64_t)0));
+        __builtin_amdgcn_sched_barrier(0);
+
+        _Float16 *ql = reinterpret_cast<_Float16 *>(smem);
+        __syncthreads();                                   // LDS of the tile before
+        // rows that do not exist keep what LDS holds: a row is one column of every product, and theirs are not stored
+#pragma unroll 1
+        for (int r = wave; r < ROWS; r += 4) {
+            float f = 0.f;
+            if (row0 + r < n_rows) f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + r, n_rows, ql, r, ROWS * QP<DH>, lane);
+            if (lane == 0) rowf[r] = f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            w.fs[rt] = rowf[16 * rt + l16];
+#pragma unroll
+            for (int p = 0; p < W::NP; ++p)
+#pragma unroll
+                for (int ks = 0; ks < L::KS; ++ks)
+                    w.qf[rt][p][ks] = *reinterpret_cast<const f16x8 *>(ql + p * ROWS * QP<DH> + (16 * rt + l16) * QP<DH> + L::dim(ks, grp));
+        }
+        w.start();
         if (b < end) {
-            int64_t slot = block_slot(g, s, h, b);
-            load_k(max(slot, (int64_t)0));
-            load_v(max(slot, (int64_t)0));
             for (;;) {
                 const bool more = b + 4 < end;
                 const int64_t next = more ? block_slot(g, s, h, b + 4) : -1;
@@ -760,16 +764,19 @@ struct Plan {
     int n_split;
     int64_t tiles;                      // workgroup row tiles per (sequence, head)
 };
-Plan plan_of(const CacheArgs &g) {
+Plan plan_of(int dtype, const CacheArgs &g) {
     Plan p;
     const int64_t rows = (int64_t)std::max(g.max_new, 1) * (g.n_heads / g.n_kv_heads);
     p.split_waves = rows <= 32;
     p.rt = rows <= 16 ? 1 : 2;
     const int per = 16 * p.rt * (p.split_waves ? 1 : 4);
     p.tiles = (rows + per - 1) / per;
-    // enough workgroups for every CU to hold several, each with at least 8 blocks of 32 keys
+    // One round of the workgroups that the CUs hold at once (a second, started round costs a whole one: 130000 tokens of
+    // 8 heads at 4 bits, 96 splits 38 us, 128 splits 47 us); two splits where the sequences alone come near a round,
+    // against their different lengths.  At least 8 blocks of 32 keys each.
+    const int64_t slots = (int64_t)CUS * (p.split_waves && p.rt == 1 && dtype == BF16 ? 3 : 2);
     const int64_t base = (int64_t)g.n_seq * g.n_kv_heads * p.tiles, blocks = ((int64_t)g.cap + 31) / 32;
-    const int64_t want = (4 * CUS + base - 1) / base, most = std::max<int64_t>(1, blocks / 8);
+    const int64_t want = base >= 2 * slots ? 1 : base > slots / 2 ? 2 : slots / base, most = std::max<int64_t>(1, blocks / 8);
     p.n_split = (int)std::min<int64_t>(std::min(want, most), MOST_SPLITS);
     return p;
 }
@@ -792,11 +799,11 @@ hipError_t run_attn(K kernel, size_t lds, const CacheArgs &g, const Plan &p, con
 
 template <int DT, int DH, int BITS>
 hipError_t run_plan(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
-    const Plan p = plan_of(g);
+    const Plan p = plan_of(DT, g);
     float *part = static_cast<float *>(ws);
     if (!p.split_waves)
         return run_attn<DT, DH>(attn_many_kernel<DT, DH, BITS>, ManyCfg<DT, DH, BITS>::LDS, g, p, y, ldy, a, part, st);
-    constexpr int OCC1 = DT == BF16 ? 3 : 2, OCC2 = 1;
+    constexpr int OCC1 = DT == BF16 ? 3 : 2, OCC2 = 2;
     return p.rt == 1 ? run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 1, OCC1>, FewCfg<DT, DH, BITS, 1>::LDS, g, p, y, ldy, a, part, st)
                      : run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 2, OCC2>, FewCfg<DT, DH, BITS, 2>::LDS, g, p, y, ldy, a, part, st);
 }
@@ -814,8 +821,8 @@ hipError_t run_dh(const CacheArgs &g, const void *y, int64_t ldy, void *a, void 
 }
 }  // namespace
 
-size_t attn_cache_ws_bytes(const CacheArgs &g) {
-    const Plan p = plan_of(g);
+size_t attn_cache_ws_bytes(int dtype, const CacheArgs &g) {
+    const Plan p = plan_of(dtype, g);
     return p.n_split == 1 ? 0 : (size_t)g.M * g.n_heads * p.n_split * (g.head_dim + 4) * sizeof(float);
 }
 

@@ -267,7 +267,7 @@ struct CacheArgs {
 // y [M][ldy] in dtype: query, key and value columns; k_out, v_out [M][n_kv_heads head_dim]
 hipError_t launch_cache_write(int dtype, const CacheArgs &g, const void *y, int64_t ldy, hipStream_t st);
 hipError_t launch_cache_read(int dtype, const CacheArgs &g, void *k_out, void *v_out, hipStream_t st);
-// a [M][n_heads head_dim] in dtype; ws: attn_cache_ws_bytes(g) (may be 0)
-size_t attn_cache_ws_bytes(const CacheArgs &g);
+// a [M][n_heads head_dim] in dtype; ws: attn_cache_ws_bytes (may be 0)
+size_t attn_cache_ws_bytes(int dtype, const CacheArgs &g);
 hipError_t launch_attn_cache(int dtype, const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st);
 }  // namespace jab
