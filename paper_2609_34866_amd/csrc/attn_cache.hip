@@ -286,17 +286,43 @@ struct Wave {
 // Queries in LDS: QP fp16 per row (padding against bank conflicts), the parts `stride` apart
 template <int DH> constexpr int QP = DH < 32 ? 40 : DH + 8;
 
+// the power of two that brings a row whose largest magnitude has the bits mx near 2^4
+__device__ inline float query_scale(uint32_t mx) {
+    const int e = min(max((int)(mx >> 23) - 127, -100), 127);
+    return pow2i(max(3 - e, -126));
+}
+// the pair (a, b) turned at a position: whole cycles are taken off the angle in fp64, the rest is fp32
+__device__ inline void turn(float &a, float &b, int pos, double freq) {
+    const double cyc = (double)pos * freq * 0.15915494309189535;
+    float sn, cs;
+    sincospif((float)(2.0 * (cyc - rint(cyc))), &sn, &cs);
+    const float x = a, y = b;
+    a = x * cs - y * sn;
+    b = y * cs + x * sn;
+}
+// a pair's fp16 parts at ql and ql + half, the next part `stride` on
+template <int NP>
+__device__ inline void query_parts(float a, float b, _Float16 *ql, int half, int stride) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const _Float16 ha = (_Float16)a, hb = (_Float16)b;
+        ql[p * stride] = ha;
+        ql[p * stride + half] = hb;
+        a -= (float)ha;
+        b -= (float)hb;
+    }
+}
+
 // One query row by one wave: turned, scaled by a power of two, as fp16 parts into row `slot` of ql; returns the
 // score scale in exp2 units with the power of two taken back (NaN for a row that is not finite)
 template <int DT, int DH, int NP>
 __device__ inline float query_row(const CacheArgs &g, const SeqRows &sr, const void *yv, int64_t ldy, int h, int G, int row,
-                                  int n_rows, _Float16 *ql, int slot, int stride, int lane) {
+                                  _Float16 *ql, int slot, int stride, int lane) {
     typedef typename Mma<DT>::elem elem;
     constexpr int HALF = DH / 2;
     float x0 = 0.f, x1 = 0.f;
-    const bool live = lane < HALF && row < n_rows;
-    const int i = live ? row / G : 0;
-    if (live) {
+    const int i = row / G;
+    if (lane < HALF) {
         const elem *q = static_cast<const elem *>(yv) + (int64_t)(sr.row + i) * ldy + ((int64_t)h * G + row % G) * DH + lane;
         x0 = to_f32<DT>(q[0]);
         x1 = to_f32<DT>(q[HALF]);
@@ -304,34 +330,70 @@ __device__ inline float query_row(const CacheArgs &g, const SeqRows &sr, const v
     uint32_t mx = max(__builtin_bit_cast(uint32_t, x0) & 0x7FFFFFFFu, __builtin_bit_cast(uint32_t, x1) & 0x7FFFFFFFu);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, off, 64));
-    const int e = min(max((int)(mx >> 23) - 127, -100), 127);                   // exponent of the largest element
-    const float up = pow2i(max(3 - e, -126));
+    const float up = query_scale(mx);
     x0 *= up;
     x1 *= up;
-    if (g.freq[0] != 0.0 && live) {
-        // whole cycles are taken off the angle in fp64, the rest is fp32
-        const double cyc = (double)(sr.past + i) * g.freq[lane] * 0.15915494309189535;
-        float sn, cs;
-        sincospif((float)(2.0 * (cyc - rint(cyc))), &sn, &cs);
-        const float a = x0, b = x1;
-        x0 = a * cs - b * sn;
-        x1 = b * cs + a * sn;
-    }
+    if (g.freq[0] != 0.0 && lane < HALF) turn(x0, x1, sr.past + i, g.freq[lane]);
     const bool fine = mx < 0x7F800000u;
-    if (lane < HALF) {
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            const _Float16 a = fine ? (_Float16)x0 : (_Float16)0.f, b = fine ? (_Float16)x1 : (_Float16)0.f;
-            ql[p * stride + slot * QP<DH> + lane] = a;
-            ql[p * stride + slot * QP<DH> + lane + HALF] = b;
-            x0 -= (float)a;
-            x1 -= (float)b;
-        }
-    }
+    _Float16 *q = ql + slot * QP<DH> + lane;
+    if (lane < HALF) query_parts<NP>(fine ? x0 : 0.f, fine ? x1 : 0.f, q, HALF, stride);
     if constexpr (DH < 32)
-        if (lane >= DH && lane < 32)
-            for (int p = 0; p < NP; ++p) ql[p * stride + slot * QP<DH> + lane] = (_Float16)0.f;
+        if (lane >= DH && lane < 32 - HALF) query_parts<NP>(0.f, 0.f, q, HALF, stride);
     return fine ? LOG2E / sqrtf((float)DH) / up : __builtin_nanf("");
+}
+
+// The same for sixteen rows row0 .. of one wave, sixteen lanes per row, into rows 0 .. 15 of ql and rowf
+template <int DT, int DH, int NP>
+__device__ inline void query_rows16(const CacheArgs &g, const SeqRows &sr, const void *yv, int64_t ldy, int h, int G, int row0,
+                                    int n_rows, _Float16 *ql, int stride, float *rowf, int lane) {
+    typedef typename Mma<DT>::elem elem;
+    constexpr int HALF = DH / 2, C = HALF / 16 < 1 ? 1 : HALF / 16;             // pairs of a lane
+    const int j0 = (lane & 15) * C;
+    const bool in = j0 < HALF;                             // head_dim 16: eight lanes per row
+    float x[4][2][C];
+    int tok[4];
+    bool live[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                          // all loads first
+        const int row = row0 + 4 * i + (lane >> 4);
+        live[i] = row < n_rows && in;
+        tok[i] = live[i] ? row / G : 0;
+        const elem *q = static_cast<const elem *>(yv) + (int64_t)(sr.row + tok[i]) * ldy + ((int64_t)h * G + (live[i] ? row % G : 0)) * DH +
+                        (in ? j0 : 0);
+        elem e[2][C];
+        __builtin_memcpy(e[0], __builtin_assume_aligned(q, C * sizeof(elem)), C * sizeof(elem));
+        __builtin_memcpy(e[1], __builtin_assume_aligned(q + HALF, C * sizeof(elem)), C * sizeof(elem));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[i][u][c] = live[i] ? to_f32<DT>(e[u][c]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t mx = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) mx = max(mx, __builtin_bit_cast(uint32_t, x[i][u][c]) & 0x7FFFFFFFu);
+        mx = max(mx, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mx, 0x128, 0xF, 0xF, false));    // row_ror 8, 4, 2, 1
+        mx = max(mx, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mx, 0x124, 0xF, 0xF, false));
+        mx = max(mx, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mx, 0x122, 0xF, 0xF, false));
+        mx = max(mx, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mx, 0x121, 0xF, 0xF, false));
+        const float up = query_scale(mx);
+        const bool fine = mx < 0x7F800000u;
+        const int slot = 4 * i + (lane >> 4);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float a = x[i][0][c] * up, b = x[i][1][c] * up;
+            if (g.freq[0] != 0.0) turn(a, b, sr.past + tok[i], g.freq[in ? j0 + c : 0]);
+            if (in)
+                query_parts<NP>(fine ? a : 0.f, fine ? b : 0.f, ql + slot * QP<DH> + j0 + c, HALF, stride);
+            else if constexpr (DH < 32) {                  // zeros behind the head: the step is 32 elements
+                query_parts<NP>(0.f, 0.f, ql + slot * QP<DH> + 16 + j0 - HALF, HALF, stride);
+            }
+        }
+        if ((lane & 15) == 0) rowf[slot] = fine ? LOG2E / sqrtf((float)DH) / up : __builtin_nanf("");
+    }
 }
 
 template <int DT>
@@ -439,7 +501,7 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
 #pragma unroll 1
         for (int r = wave; r < ROWS; r += 4) {
             float f = 0.f;
-            if (row0 + r < n_rows) f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + r, n_rows, ql, r, ROWS * QP<DH>, lane);
+            if (row0 + r < n_rows) f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + r, ql, r, ROWS * QP<DH>, lane);
             if (lane == 0) rowf[r] = f;
         }
         __syncthreads();
@@ -538,18 +600,22 @@ struct ManyCfg {
 
 template <int DT, int DH, int BITS>
 __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy,
-                                                           void *__restrict__ av, float *__restrict__ part, int n_split) {
+                                                           void *__restrict__ av, float *__restrict__ part, int n_split,
+                                                           int tiles) {
     typedef ManyCfg<DT, DH, BITS> S;
     typedef Wave<DT, DH, BITS, S::RT> W;
     typedef Lay<DH, BITS> L;
     constexpr int QMID = (1 << (BITS - 1)) - 1, RT = S::RT;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float rowf[64];
-    __shared__ int has[2][2];                              // per stage and block: its page exists
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l16 = lane & 15, grp = lane >> 4;
-    const int split = blockIdx.x % n_split, sh = blockIdx.x / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
+    // grid: `tiles` row tiles of each (sequence, key/value head, split), eight of these at a time: workgroups whose
+    // ids are congruent mod 8 run on one XCD, so the tiles that read the same keys share its L2
+    const int item = (int)(blockIdx.x / (8u * tiles)) * 8 + (int)(blockIdx.x & 7), tile0 = (int)(blockIdx.x / 8u % (uint32_t)tiles);
+    const int split = item % n_split, sh = item / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
+    if (s >= g.n_seq) return;
     const SeqRows sr = seq_rows(g, s);
     const int G = g.n_heads / g.n_kv_heads;
     const int n_rows = sr.n * G, n_tiles = (n_rows + S::ROWS - 1) / S::ROWS;
@@ -557,9 +623,11 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
     const int b0 = (int)((int64_t)n_blk * split / n_split), b1 = (int)((int64_t)n_blk * (split + 1) / n_split);
     const bool asym = g.k_zero != nullptr;
     const int kind = wave >> 1, mine = wave & 1;           // what this wave prepares: keys or values, of which block
+    const uint8_t *code_base = kind ? g.v : g.k, *zero_base = kind ? g.v_zero : g.k_zero;
+    const uint8_t *scale_base = reinterpret_cast<const uint8_t *>(kind ? g.v_scale : g.k_scale);
 
     // the last tiles see the most keys: first
-    for (int tile = n_tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= gridDim.y) {
+    for (int tile = n_tiles - 1 - tile0; tile >= 0; tile -= tiles) {
         const int row0 = tile * S::ROWS + wave * 16 * RT;
         W w;
         _Float16 *ql = reinterpret_cast<_Float16 *>(smem) + wave * 16 * QP<DH>;
@@ -567,11 +635,7 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             __syncthreads();                               // LDS of the tile before, and of the rows before
-#pragma unroll 1
-            for (int r = 0; r < 16; ++r) {
-                const float f = query_row<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + 16 * rt + r, n_rows, ql, r, QSTRIDE, lane);
-                if (lane == 0) rowf[wave * 16 + r] = f;
-            }
+            query_rows16<DT, DH, W::NP>(g, sr, yv, ldy, h, G, row0 + 16 * rt, n_rows, ql, QSTRIDE, rowf + wave * 16, lane);
             __syncthreads();
             w.fs[rt] = rowf[wave * 16 + l16];
 #pragma unroll
@@ -589,26 +653,25 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
         u32x2 raw[2 * L::KU > L::VU ? 2 * L::KU : L::VU], vz = {0, 0};
         int kz[2] = {QMID, QMID};
         float sc = 0.f;
-        int64_t slot = -1;
         const uint32_t zoff = L::key(0, l16), koff = zoff * L::DHB + L::kbyte(0, grp), voff = L::vrow(0, l16) * 32 + 8 * grp;
-        auto load = [&](int b) {                           // this wave's share of blocks b, b + 1
-            slot = b + mine < end ? block_slot(g, s, h, b + mine) : -1;
-            const int64_t at = max(slot, (int64_t)0);
+        auto page_at = [&](int b) { return b < end ? page_of(g, s, b * 32) : -1; };
+        auto load = [&](int b, int page) {                 // this wave's share of a stage: of block b, in that page
+            const int64_t at = (((int64_t)max(page, 0) * g.n_kv_heads + h) << g.page_shift) +
+                               ((b * 32) & ((1 << g.page_shift) - 1));
+            const uint8_t *codes = code_base + at * L::DHB;
             if (kind == 0) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                    for (int u = 0; u < L::KU; ++u)
-                        raw[t * L::KU + u] = ldu<u32x2>(g.k + at * L::DHB, koff + 4 * t * L::DHB + L::kbyte(u, 0));
-                    if (asym) kz[t] = ldu<uint8_t>(g.k_zero + at, zoff + 4 * t);
+                    for (int u = 0; u < L::KU; ++u) raw[t * L::KU + u] = ldu<u32x2>(codes, koff + 4 * t * L::DHB + L::kbyte(u, 0));
+                    if (asym) kz[t] = ldu<uint8_t>(zero_base + at, zoff + 4 * t);
                 }
-                sc = ldu<float>(reinterpret_cast<const uint8_t *>(g.k_scale + at), 4 * (lane & 31));
             } else {
 #pragma unroll
-                for (int u = 0; u < L::VU; ++u) raw[u] = ldu<u32x2>(g.v + at * L::DHB, voff + 512 * u);
-                if (asym) vz = ldu<u32x2>(g.v_zero + at, 8 * grp);
-                sc = ldu<float>(reinterpret_cast<const uint8_t *>(g.v_scale + at), 4 * (lane & 31));
+                for (int u = 0; u < L::VU; ++u) raw[u] = ldu<u32x2>(codes, voff + 512 * u);
+                if (asym) vz = ldu<u32x2>(zero_base + at, 8 * grp);
             }
+            sc = ldu<float>(scale_base + 4 * at, 4 * (lane & 31));
         };
         auto prepare = [&](int buf) {                      // into stage buf
             unsigned char *blk = smem + buf * S::STAGE + mine * S::BLOCK;
@@ -623,7 +686,6 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
                     for (int ks = 0; ks < L::KS; ++ks)
                         *reinterpret_cast<f16x8 *>(blk + (t * L::KS + ks) * 1024 + lane * 16) = L::kop(k, ks, grp, z);
                 }
-                if (lane == 0) has[buf][mine] = slot >= 0;
             } else {
                 f16x2 z[4] = {biased(vz[0], false), biased(vz[0], true), biased(vz[1], false), biased(vz[1], true)};
                 if (!asym) z[0] = z[1] = z[2] = z[3] = both(QMID);
@@ -636,16 +698,18 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
             }
             if (lane < 32) *reinterpret_cast<float *>(blk + S::OPS * 1024 + kind * 128 + lane * 4) = sc;
         };
-        int buf = 0;
-        if (b0 < end) load(b0);
+        // page numbers (scalar loads) two stages ahead, bytes one stage ahead
+        int buf = 0, pg[2] = {page_at(b0), page_at(b0 + 1)}, pn[2] = {page_at(b0 + 2), page_at(b0 + 3)};
+        if (b0 < end) load(b0 + mine, mine ? pg[1] : pg[0]);
         for (int b = b0; b < end; b += 2) {
+            const int pf[2] = {page_at(b + 4), page_at(b + 5)};
             prepare(buf);
-            if (b + 2 < end) load(b + 2);
+            if (b + 2 < end) load(b + 2 + mine, mine ? pn[1] : pn[0]);
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const unsigned char *blk = smem + buf * S::STAGE + i * S::BLOCK;
-                if ((b + i) * 32 > w.hi_lim || b + i >= end || !__builtin_amdgcn_readfirstlane(has[buf][i])) continue;
+                if (pg[i] < 0 || (b + i) * 32 > w.hi_lim) continue;             // no page (or past the end), or past this wave's rows
                 const int key0 = (b + i) * 32 + 8 * grp;
                 const bool edge = (b + i) * 32 + 31 > w.lo_lim;
                 const f32x4 *scl = reinterpret_cast<const f32x4 *>(blk + S::OPS * 1024);
@@ -658,6 +722,11 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
                 w.values(pw, [&](int t) { return *reinterpret_cast<const f16x8 *>(blk + (S::KOPS + t) * 1024 + lane * 16); });
             }
             buf ^= 1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                pg[i] = pn[i];
+                pn[i] = pf[i];
+            }
         }
         w.finish();
 #pragma unroll
@@ -757,6 +826,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(CacheArgs g, const float
 }
 
 constexpr int CUS = 256;
+constexpr int64_t MOST_GROUPS = 1 << 23; // workgroups of one launch (a grid has below 2^32 threads)
 // Rows of one key/value head, the wave arrangement and the splits of the key axis.
 struct Plan {
     bool split_waves;                   // the waves of a workgroup share their rows
@@ -781,13 +851,12 @@ Plan plan_of(int dtype, const CacheArgs &g) {
     return p;
 }
 
-template <int DT, int DH, typename K>
-hipError_t run_attn(K kernel, size_t lds, const CacheArgs &g, const Plan &p, const void *y, int64_t ldy, void *a, float *part,
-                    hipStream_t st) {
+template <int DT, int DH, typename K, typename... A>
+hipError_t run_attn(K kernel, size_t lds, dim3 grid, const CacheArgs &g, const Plan &p, const void *y, int64_t ldy, void *a,
+                    float *part, hipStream_t st, A... more) {
     hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    const dim3 grid((unsigned)(g.n_seq * g.n_kv_heads * p.n_split), (unsigned)std::min<int64_t>(p.tiles, 65535));
-    kernel<<<grid, 256, lds, st>>>(g, y, ldy, a, part, p.n_split);
+    kernel<<<grid, 256, lds, st>>>(g, y, ldy, a, part, p.n_split, more...);
     e = hipGetLastError();
     if (e != hipSuccess || p.n_split == 1) return e;
     const int64_t items = (int64_t)std::max(g.max_new, 1) * g.n_heads;
@@ -801,11 +870,17 @@ template <int DT, int DH, int BITS>
 hipError_t run_plan(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
     const Plan p = plan_of(DT, g);
     float *part = static_cast<float *>(ws);
-    if (!p.split_waves)
-        return run_attn<DT, DH>(attn_many_kernel<DT, DH, BITS>, ManyCfg<DT, DH, BITS>::LDS, g, p, y, ldy, a, part, st);
+    const int64_t items = (int64_t)g.n_seq * g.n_kv_heads * p.n_split;
+    if (!p.split_waves) {
+        const int64_t eights = (items + 7) / 8 * 8;
+        const int tiles = (int)std::max<int64_t>(1, std::min(p.tiles, MOST_GROUPS / eights));
+        return run_attn<DT, DH>(attn_many_kernel<DT, DH, BITS>, ManyCfg<DT, DH, BITS>::LDS, dim3((unsigned)(eights * tiles)), g, p,
+                                y, ldy, a, part, st, tiles);
+    }
     constexpr int OCC1 = DT == BF16 ? 3 : 2, OCC2 = 2;
-    return p.rt == 1 ? run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 1, OCC1>, FewCfg<DT, DH, BITS, 1>::LDS, g, p, y, ldy, a, part, st)
-                     : run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 2, OCC2>, FewCfg<DT, DH, BITS, 2>::LDS, g, p, y, ldy, a, part, st);
+    const dim3 grid((unsigned)items, (unsigned)p.tiles);
+    return p.rt == 1 ? run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 1, OCC1>, FewCfg<DT, DH, BITS, 1>::LDS, grid, g, p, y, ldy, a, part, st)
+                     : run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 2, OCC2>, FewCfg<DT, DH, BITS, 2>::LDS, grid, g, p, y, ldy, a, part, st);
 }
 template <int DT, int DH>
 hipError_t run_bits(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
