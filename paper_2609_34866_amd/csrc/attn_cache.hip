@@ -401,17 +401,150 @@ __device__ inline void store4(typename Mma<DT>::elem *p, f32x4 v) {
     if constexpr (DT == F32) *reinterpret_cast<f32x4 *>(p) = v;
     else *reinterpret_cast<u32x2 *>(p) = u32x2{pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
 }
-// four elements d .. d + 3 of a row: the output, or the split's share of it (O, m, l)
+// ---------------------------------------------------------------- shares
+// The work is a list of blocks of 32 keys: for each key/value head, sequence and tile of ROWS query rows, the blocks
+// up to the last position that the tile sees.  It is cut in equal shares, one per workgroup, wherever the
+// sequences' lengths put the cuts (only the device knows them), so no workgroup is left with a long sequence.
+// A cut closer than SNAP blocks to a tile's end moves there.  A tile that lies in one share is written as output;
+// a share has at most two pieces of others, its first (slot 0: the tile began in an earlier share) and its last (slot 1:
+// the tile begins here), which attn_join_kernel joins.
+constexpr int SNAP = 8, SHARE = 8;      // least blocks of a piece, of a share
+constexpr int SCAN_SEQS = 512;          // sequences up to which each workgroup scans them; past it one workgroup per
+                                        // (sequence, head), of which there are then enough
+constexpr int WHOLE = 48;               // blocks below which a (sequence, head) goes to one workgroup
+
+template <int ROWS>
+__device__ inline int tile_blocks(const CacheArgs &g, const SeqRows &r, int G, int tile) {
+    const int end = (tile + 1) * ROWS, tok = end >= r.n * G ? r.n - 1 : (end - 1) / G;
+    return (min(r.past + tok, g.cap - 1) >> 5) + 1;
+}
+// blocks of one head of a sequence
+template <int ROWS>
+__device__ inline uint32_t head_blocks(const CacheArgs &g, const SeqRows &r, int G) {
+    uint32_t sum = 0;
+    for (int t = 0; t * ROWS < r.n * G; ++t) sum += tile_blocks<ROWS>(g, r, G, t);
+    return sum;
+}
+// inclusive sum over the wave's lanes: rows of 16 by shifts, then the rows before
+__device__ inline uint32_t wave_scan(uint32_t v) {
+    auto add = [&](auto ctrl, auto rows) {
+        v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    };
+    typedef std::integral_constant<int, 0xF> all;
+    add(std::integral_constant<int, 0x111>(), all());      // row_shr 1, 2, 4, 8
+    add(std::integral_constant<int, 0x112>(), all());
+    add(std::integral_constant<int, 0x114>(), all());
+    add(std::integral_constant<int, 0x118>(), all());
+    add(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());      // row_bcast 15 into rows 1, 3
+    add(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());      // row_bcast 31 into rows 2, 3
+    return v;
+}
+__device__ inline uint32_t lane_value(uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); }
+
+struct Piece {                          // what a slot holds
+    int s, h, tile;
+    int flag;                           // 0 nothing, 1 a part, 2 the part that ends the tile
+};
+
+// The workgroup's share: where it starts and its blocks (wave-uniform; a head's blocks of all sequences stay below
+// 2^31).  SCAN: equal shares; else a (sequence, head) per workgroup.
+template <int ROWS, bool SCAN>
+struct Share {
+    int s, h, tile, blk;
+    int64_t left;
+
+    __device__ inline void advance(const CacheArgs &g, int G) {        // to the start of the next tile
+        blk = 0;
+        if (++tile * ROWS < seq_rows(g, s).n * G) return;
+        tile = 0;
+#pragma unroll 1
+        for (int k = 0; k <= g.n_seq; ++k) {               // the next sequence with new tokens, or the next head's first
+            if (++s == g.n_seq) {
+                s = 0;
+                ++h;
+            }
+            if (seq_rows(g, s).n > 0) return;
+        }
+    }
+    __device__ inline void find(const CacheArgs &g, int G, int share, int n_shares, int lane) {
+        left = 0;
+        if constexpr (!SCAN) {
+            s = share / g.n_kv_heads;
+            h = share - s * g.n_kv_heads;
+            tile = blk = 0;
+            const SeqRows r = seq_rows(g, s);
+#pragma unroll 1
+            for (int t = 0; t * ROWS < r.n * G; ++t) left += tile_blocks<ROWS>(g, r, G, t);
+            return;
+        }
+        // lane i: the blocks of sequences i per .. (i + 1) per - 1
+        const int per = (g.n_seq + 63) / 64;
+        uint32_t sum = 0;
+#pragma unroll 1
+        for (int i = lane * per; i < min((lane + 1) * per, g.n_seq); ++i) sum += head_blocks<ROWS>(g, seq_rows(g, i), G);
+        const uint32_t inc = wave_scan(sum), total = lane_value(inc, 63);
+        if (total == 0) return;
+        const int n = (int)min((int64_t)n_shares, max((int64_t)total * g.n_kv_heads / SHARE, (int64_t)1));
+        if (share >= n) return;
+        const double step = (double)total / n;             // a cut is the same number for the shares on both its sides
+        int64_t to = 0;
+#pragma unroll 1
+        for (int e = 1; e >= 0; --e) {                     // where the share ends, then where it starts
+            const uint32_t u = (uint32_t)(share + e) * (uint32_t)g.n_kv_heads;
+            h = (int)(u / (uint32_t)n);
+            uint32_t x = min((uint32_t)((double)(u - (uint32_t)h * n) * step), total - 1);
+            int64_t at = (int64_t)h * total + x;
+            s = tile = blk = 0;
+            if (h < g.n_kv_heads) {
+                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(inc > x));
+                x -= l ? lane_value(inc, l - 1) : 0u;
+                s = l * per;
+                SeqRows r = seq_rows(g, s);
+                uint32_t nb = r.n > 0 ? tile_blocks<ROWS>(g, r, G, 0) : 0;
+                const int stop = min((l + 1) * per, g.n_seq) - 1;
+#pragma unroll 1
+                while (x >= nb) {                          // the next tile, of the lane's next sequence after the last one
+                    x -= nb;
+                    if (++tile * ROWS >= r.n * G) {
+                        if (s == stop) break;              // (never, unless the tables change under the call)
+                        tile = 0;
+                        r = seq_rows(g, ++s);
+                    }
+                    nb = r.n > 0 ? tile_blocks<ROWS>(g, r, G, tile) : 0;
+                }
+                blk = (int)x;
+                if (blk < SNAP) {
+                    at -= blk;
+                    blk = 0;
+                } else if ((int)nb - blk < SNAP) {
+                    at += (int)nb - blk;
+                    advance(g, G);
+                }
+            }
+            if (e) to = at;
+            else left = to - at;
+        }
+    }
+};
+
+// workgroup -> share: an XCD (ids congruent mod 8) takes a contiguous range, so that tiles that read the same keys share
+// its L2
+__device__ inline int share_of(int block, int n_shares) {
+    return (n_shares & 7) == 0 ? (block & 7) * (n_shares >> 3) + (block >> 3) : block;
+}
+
+// four elements d .. d + 3 of a row: the output, or (part: the slot's rows, [row][DH + 4]: O, m, l) a piece of it
 template <int DT, int DH>
-__device__ inline void put_row(const CacheArgs &g, const SeqRows &sr, int h, int G, int row, int d, f32x4 v, float m, float l,
-                               void *av, float *part, int split, int n_split) {
+__device__ inline void put_row(const CacheArgs &g, const SeqRows &sr, int h, int G, int row0, int r, int d, f32x4 v, float m, float l,
+                               void *av, float *part) {
     typedef typename Mma<DT>::elem elem;
-    const int64_t at = (int64_t)(sr.row + row / G) * g.n_heads + (int64_t)h * G + row % G;
-    if (n_split == 1) {
+    if (part == nullptr) {
+        const int row = row0 + r;
+        const int64_t at = (int64_t)(sr.row + row / G) * g.n_heads + (int64_t)h * G + row % G;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         store4<DT>(static_cast<elem *>(av) + at * DH + d, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
     } else {
-        float *pp = part + (at * n_split + split) * (DH + 4);
+        float *pp = part + r * (DH + 4);
         *reinterpret_cast<f32x4 *>(pp + d) = v;
         if (d == 0) {
             pp[DH] = m;
@@ -431,10 +564,10 @@ struct FewCfg {
     static constexpr size_t LDS = Q_LDS > O_LDS ? Q_LDS : O_LDS;
 };
 
-// grid: x = (sequence, key/value head, split), y = row tiles (dealt out)
-template <int DT, int DH, int BITS, int RT, int OCC>
+template <int DT, int DH, int BITS, int RT, int OCC, bool SCAN>
 __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy,
-                                                          void *__restrict__ av, float *__restrict__ part, int n_split) {
+                                                          void *__restrict__ av, float *__restrict__ parts,
+                                                          Piece *__restrict__ pieces) {
     typedef Wave<DT, DH, BITS, RT> W;
     typedef Lay<DH, BITS> L;
     constexpr int QMID = (1 << (BITS - 1)) - 1, ROWS = 16 * RT;
@@ -444,18 +577,28 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l16 = lane & 15, grp = lane >> 4;
-    const int split = blockIdx.x % n_split, sh = blockIdx.x / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
-    const SeqRows sr = seq_rows(g, s);
     const int G = g.n_heads / g.n_kv_heads;
-    const int n_rows = sr.n * G;
-    const int len = (int)min((int64_t)sr.past + sr.n, (int64_t)g.cap), n_blk = (len + 31) >> 5;
-    const int b0 = (int)((int64_t)n_blk * split / n_split), b1 = (int)((int64_t)n_blk * (split + 1) / n_split);
     const bool asym = g.k_zero != nullptr;
+    const int share = SCAN ? share_of(blockIdx.x, gridDim.x) : blockIdx.x;
+    Share<ROWS, SCAN> sh;
+    sh.find(g, G, share, gridDim.x, lane);
+    if (SCAN && threadIdx.x == 0) pieces[2 * share].flag = pieces[2 * share + 1].flag = 0;
 
-    for (int tile = blockIdx.y, row0; (row0 = tile * ROWS) < n_rows; tile += gridDim.y) {
+    while (sh.left > 0 && sh.h < g.n_kv_heads) {
+        const int s = sh.s, h = sh.h;
+        const SeqRows sr = seq_rows(g, s);
+        const int n_rows = sr.n * G, row0 = sh.tile * ROWS, nb = tile_blocks<ROWS>(g, sr, G, sh.tile);
+        const int b0 = sh.blk, end = (int)min(b0 + sh.left, (int64_t)nb);
+        float *part = nullptr;
+        if (SCAN && (b0 > 0 || end < nb)) {
+            const int slot = 2 * share + (b0 == 0);
+            part = parts + (int64_t)slot * ROWS * (DH + 4);
+            if (threadIdx.x == 0) pieces[slot] = Piece{s, h, sh.tile, end < nb ? 1 : 2};
+        }
+        sh.left -= end - b0;
+        sh.advance(g, G);
         W w;
         w.limits(g, sr, G, row0, n_rows, l16);
-        const int end = min(b1, (w.hi_lim >> 5) + 1);
         u32x2 k[2][L::KU], v[L::VU], vz = {0, 0};
         f32x4 ks[2], vs[2];
         int kz[2] = {QMID, QMID};
@@ -487,7 +630,7 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
             for (int t = 0; t < 2; ++t) vs[t] = ldu<f32x4>(sb, 32 * grp + 16 * t);
             if (asym) vz = ldu<u32x2>(g.v_zero + slot, 8 * grp);
         };
-        // blocks wave, wave + 4, ... of the split, the first one's bytes on their way before the queries are made; a
+        // blocks wave, wave + 4, ... of the piece, the first one's bytes on their way before the queries are made; a
         // block without a page, and past the end, loads page 0 and is not used
         int b = b0 + wave;
         int64_t slot = b < end ? block_slot(g, s, h, b) : -1;
@@ -577,7 +720,7 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
                 for (int e = 0; e < 4; ++e) sum[e] += f * x[e];
                 ll += f * ml[i][r][1];
             }
-            put_row<DT, DH>(g, sr, h, G, row0 + r, d, sum, mm, ll, av, part, split, n_split);
+            put_row<DT, DH>(g, sr, h, G, row0, r, d, sum, mm, ll, av, part);
         }
     }
 }
@@ -598,10 +741,10 @@ struct ManyCfg {
     static constexpr size_t LDS = 2 * STAGE > Q_LDS ? 2 * STAGE : Q_LDS;
 };
 
-template <int DT, int DH, int BITS>
+template <int DT, int DH, int BITS, bool SCAN>
 __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy,
-                                                           void *__restrict__ av, float *__restrict__ part, int n_split,
-                                                           int tiles) {
+                                                           void *__restrict__ av, float *__restrict__ parts,
+                                                           Piece *__restrict__ pieces) {
     typedef ManyCfg<DT, DH, BITS> S;
     typedef Wave<DT, DH, BITS, S::RT> W;
     typedef Lay<DH, BITS> L;
@@ -611,24 +754,29 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l16 = lane & 15, grp = lane >> 4;
-    // grid: `tiles` row tiles of each (sequence, key/value head, split), eight of these at a time: workgroups whose
-    // ids are congruent mod 8 run on one XCD, so the tiles that read the same keys share its L2
-    const int item = (int)(blockIdx.x / (8u * tiles)) * 8 + (int)(blockIdx.x & 7), tile0 = (int)(blockIdx.x / 8u % (uint32_t)tiles);
-    const int split = item % n_split, sh = item / n_split, h = sh % g.n_kv_heads, s = sh / g.n_kv_heads;
-    if (s >= g.n_seq) return;
-    const SeqRows sr = seq_rows(g, s);
     const int G = g.n_heads / g.n_kv_heads;
-    const int n_rows = sr.n * G, n_tiles = (n_rows + S::ROWS - 1) / S::ROWS;
-    const int len = (int)min((int64_t)sr.past + sr.n, (int64_t)g.cap), n_blk = (len + 31) >> 5;
-    const int b0 = (int)((int64_t)n_blk * split / n_split), b1 = (int)((int64_t)n_blk * (split + 1) / n_split);
     const bool asym = g.k_zero != nullptr;
     const int kind = wave >> 1, mine = wave & 1;           // what this wave prepares: keys or values, of which block
     const uint8_t *code_base = kind ? g.v : g.k, *zero_base = kind ? g.v_zero : g.k_zero;
     const uint8_t *scale_base = reinterpret_cast<const uint8_t *>(kind ? g.v_scale : g.k_scale);
+    const int share = SCAN ? share_of(blockIdx.x, gridDim.x) : blockIdx.x;
+    Share<S::ROWS, SCAN> sh;
+    sh.find(g, G, share, gridDim.x, lane);
+    if (SCAN && threadIdx.x == 0) pieces[2 * share].flag = pieces[2 * share + 1].flag = 0;
 
-    // the last tiles see the most keys: first
-    for (int tile = n_tiles - 1 - tile0; tile >= 0; tile -= tiles) {
-        const int row0 = tile * S::ROWS + wave * 16 * RT;
+    while (sh.left > 0 && sh.h < g.n_kv_heads) {
+        const int s = sh.s, h = sh.h;
+        const SeqRows sr = seq_rows(g, s);
+        const int n_rows = sr.n * G, tile0 = sh.tile * S::ROWS, row0 = tile0 + wave * 16 * RT;
+        const int nb = tile_blocks<S::ROWS>(g, sr, G, sh.tile), b0 = sh.blk, end = (int)min(b0 + sh.left, (int64_t)nb);
+        float *part = nullptr;
+        if (SCAN && (b0 > 0 || end < nb)) {
+            const int slot = 2 * share + (b0 == 0);
+            part = parts + (int64_t)slot * S::ROWS * (DH + 4);
+            if (threadIdx.x == 0) pieces[slot] = Piece{s, h, sh.tile, end < nb ? 1 : 2};
+        }
+        sh.left -= end - b0;
+        sh.advance(g, G);
         W w;
         _Float16 *ql = reinterpret_cast<_Float16 *>(smem) + wave * 16 * QP<DH>;
         constexpr int QSTRIDE = 4 * 16 * QP<DH>;
@@ -647,8 +795,6 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
         __syncthreads();                                   // the stages lie over the queries
         w.limits(g, sr, G, row0, n_rows, l16);
         w.start();
-        const int last = min((tile + 1) * S::ROWS, n_rows) - 1;
-        const int end = min(b1, (min(sr.past + last / G, g.cap - 1) >> 5) + 1);   // of the workgroup's rows
 
         u32x2 raw[2 * L::KU > L::VU ? 2 * L::KU : L::VU], vz = {0, 0};
         int kz[2] = {QMID, QMID};
@@ -735,152 +881,174 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
             if (row < n_rows)
 #pragma unroll
                 for (int t = 0; t < L::NT; ++t)
-                    put_row<DT, DH>(g, sr, h, G, row, 16 * t + 4 * grp, w.o[rt][t], w.m[rt], w.l[rt], av, part, split, n_split);
+                    put_row<DT, DH>(g, sr, h, G, tile0, row - tile0, 16 * t + 4 * grp, w.o[rt][t], w.m[rt], w.l[rt], av, part);
         }
     }
 }
 
-// The splits of a row joined; part [row][split][DH + 4]: O, m, l.  LANES threads per (token, head): a wave where
-// there are few splits (and then many rows), else a workgroup, so that all of a row's loads are in flight at once.
-constexpr int MOST_SPLITS = 128;
-template <int DT, int DH, int LANES>
-__global__ __launch_bounds__(256) void attn_join_kernel(CacheArgs g, const float *__restrict__ part, void *__restrict__ av,
-                                                        int n_split) {
-    typedef typename Mma<DT>::elem elem;
-    constexpr int LPR = DH / 4, SG = LANES / LPR, RPB = 256 / LANES;             // lanes of a row's elements, splits at once
-    constexpr int WS = LANES / 64;                                               // waves of a row
-    __shared__ float fac[RPB][MOST_SPLITS];
-    __shared__ float2 ml[RPB][WS];
-    __shared__ f32x4 sum[WS][LPR];
-    const int tid = threadIdx.x % LANES, lane = threadIdx.x & 63;
-    const int r = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / LANES)), wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int s = blockIdx.x;
-    const SeqRows sr = seq_rows(g, s);
-    const int64_t items = (int64_t)sr.n * g.n_heads;
-    const int d = tid % LPR * 4, sg = tid / LPR;
-    for (int64_t it0 = (int64_t)blockIdx.y * RPB; it0 < items; it0 += (int64_t)gridDim.y * RPB) {
-        const int64_t it = min(it0 + r, items - 1), row = (int64_t)sr.row * g.n_heads + it;     // (the last row twice: same values)
-        const float *p = part + row * n_split * (DH + 4);
-        // thread i the factor of split i (two for a wave of 64)
-        float mi[(MOST_SPLITS + LANES - 1) / LANES], li[(MOST_SPLITS + LANES - 1) / LANES], m = -__builtin_inff(), l = 0.f;
+// The pieces of the tile that begins in share blockIdx.x and ends in a later one: a wave per row for few pieces, else a
+// workgroup, so that a row's loads are in flight together.
+constexpr int CUS = 256;
+constexpr int MOST_SHARES = 3 * CUS;
+template <int DT, int DH, int ROWS>
+__global__ __launch_bounds__(256) void attn_join_kernel(CacheArgs g, const float *__restrict__ parts,
+                                                        const Piece *__restrict__ pieces, int n_shares, void *__restrict__ av) {
+    constexpr int LPR = DH / 4, PITCH = DH + 4;            // lanes of a row's elements
+    __shared__ int last_share;
+    __shared__ float fac[MOST_SHARES], red[4][2];
+    __shared__ f32x4 sum[4][LPR];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int w = blockIdx.x;
+    const Piece p = pieces[2 * w + 1];
+    if (p.flag != 1) return;
+    if (tid == 0) last_share = n_shares;
+    __syncthreads();
+    for (int i = w + 1 + tid; i < n_shares; i += 256)      // the first end behind it is its own
+        if (pieces[2 * i].flag == 2) {
+            atomicMin(&last_share, i);
+            break;
+        }
+    __syncthreads();
+    const int count = last_share - w + 1;                  // pieces: slot 2 w + 1, then 2 (w + 1), 2 (w + 2), ...
+    if (last_share == n_shares) return;
+    const SeqRows sr = seq_rows(g, p.s);
+    const int G = g.n_heads / g.n_kv_heads, row0 = p.tile * ROWS, live = min(ROWS, sr.n * G - row0);
+    auto piece = [&](int i, int r) { return parts + ((int64_t)(i ? 2 * (w + i) : 2 * w + 1) * ROWS + r) * PITCH; };
+    if (count <= 8) {                                      // LPR lanes per row, every row's loads in flight at once
+        constexpr int RPW = 64 / LPR, STEP = 2;
+        const int d = lane % LPR * 4, step = 4 * RPW * gridDim.y;
+        for (int r0 = (blockIdx.y * 4 + wave) * RPW + lane / LPR; r0 < live; r0 += STEP * step) {
 #pragma unroll
-        for (int k = 0; k < (MOST_SPLITS + LANES - 1) / LANES; ++k) {
-            const int i = tid + k * LANES;
-            mi[k] = i < n_split ? p[(int64_t)i * (DH + 4) + DH] : -__builtin_inff();
-            li[k] = i < n_split ? p[(int64_t)i * (DH + 4) + DH + 1] : 0.f;
+            for (int u = 0; u < STEP; ++u) {
+                const int r = r0 + u * step, rr = min(r, live - 1);
+                float m = -__builtin_inff(), l = 0.f;
+                f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < count; ++i) {          // the reference moves with the larger m
+                    const float *q = piece(i, rr);
+                    const float mi = q[DH], li = q[DH + 1];
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(q + d);
+                    const float mn = fmaxf(m, mi), a = m == mn ? 1.f : exp2f(m - mn), b = mi == mn ? 1.f : exp2f(mi - mn);
+                    m = mn;
+                    l = a * l + b * li;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = a * v[k] + b * x[k];
+                }
+                if (r < live) put_row<DT, DH>(g, sr, p.h, G, row0, r, d, v, m, l, av, nullptr);
+            }
+        }
+        return;
+    }
+    constexpr int SG = 256 / LPR;
+    const int d = tid % LPR * 4, sg = tid / LPR;
+    for (int r = blockIdx.y; r < live; r += gridDim.y) {
+        float mi[MOST_SHARES / 256], li[MOST_SHARES / 256], m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+        for (int k = 0; k < MOST_SHARES / 256; ++k) {
+            const int i = tid + 256 * k;
+            mi[k] = i < count ? piece(i, r)[DH] : -__builtin_inff();
+            li[k] = i < count ? piece(i, r)[DH + 1] : 0.f;
             m = fmaxf(m, mi[k]);
         }
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-        if constexpr (WS > 1) {
-            __syncthreads();                               // the row before is done with ml, fac and sum
-            if (lane == 0) ml[r][wv].x = m;
-            __syncthreads();
+        __syncthreads();                                   // the row before is done with red, fac and sum
+        if (lane == 0) red[wave][0] = m;
+        __syncthreads();
 #pragma unroll
-            for (int w = 0; w < WS; ++w) m = fmaxf(m, ml[r][w].x);
-        }
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, red[i][0]);
 #pragma unroll
-        for (int k = 0; k < (MOST_SPLITS + LANES - 1) / LANES; ++k) {
-            const int i = tid + k * LANES;
+        for (int k = 0; k < MOST_SHARES / 256; ++k) {
+            const int i = tid + 256 * k;
             const float f = mi[k] == m ? 1.f : exp2f(mi[k] - m);
-            if (i < n_split) fac[r][i] = f;
+            if (i < count) fac[i] = f;
             l += f * li[k];
         }
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off, 64);
-        if (WS > 1 && lane == 0) ml[r][wv].y = l;
+        if (lane == 0) red[wave][1] = l;
         __syncthreads();
-        if constexpr (WS > 1) {
-            l = 0.f;
-#pragma unroll
-            for (int w = 0; w < WS; ++w) l += ml[r][w].y;
-        }
+        l = red[0][1] + red[1][1] + red[2][1] + red[3][1];
         f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-        for (int i = sg; i < n_split; i += SG) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(p + (int64_t)i * (DH + 4) + d);
-            const float f = fac[r][i];
+        for (int i = sg; i < count; i += SG) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(piece(i, r) + d);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] += f * x[k];
+            for (int k = 0; k < 4; ++k) v[k] += fac[i] * x[k];
         }
 #pragma unroll
         for (int off = 32; off >= LPR; off >>= 1)
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] += __shfl_xor(v[k], off, 64);
-        if constexpr (WS > 1) {
-            if (lane < LPR) sum[wv][lane] = v;
-            __syncthreads();
-            if (tid < LPR) {
-                v = sum[0][tid];
-#pragma unroll
-                for (int w = 1; w < WS; ++w)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] += sum[w][tid][k];
-            }
-        }
+        if (lane < LPR) sum[wave][lane] = v;
+        __syncthreads();
         if (tid < LPR) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            store4<DT>(static_cast<elem *>(av) + row * DH + d, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = (sum[0][tid][k] + sum[1][tid][k]) + (sum[2][tid][k] + sum[3][tid][k]);
+            put_row<DT, DH>(g, sr, p.h, G, row0, r, d, v, m, l, av, nullptr);
         }
     }
 }
 
-constexpr int CUS = 256;
-constexpr int64_t MOST_GROUPS = 1 << 23; // workgroups of one launch (a grid has below 2^32 threads)
-// Rows of one key/value head, the wave arrangement and the splits of the key axis.
+// The kernel and its shares, from the sizes that the host knows.
 struct Plan {
-    bool split_waves;                   // the waves of a workgroup share their rows
-    int rt;                             // 16-row tiles per wave
-    int n_split;
-    int64_t tiles;                      // workgroup row tiles per (sequence, head)
+    bool few, scan;                     // scan: equal shares of the whole batch, whose pieces are joined
+    bool many_pieces;                   // tiles of more than 8 shares are expected
+    int rt, rows;                       // few: 16-row tiles of a wave; rows of a tile
+    int groups;                         // workgroups = shares
 };
 Plan plan_of(int dtype, const CacheArgs &g) {
     Plan p;
-    const int64_t rows = (int64_t)std::max(g.max_new, 1) * (g.n_heads / g.n_kv_heads);
-    p.split_waves = rows <= 32;
+    const int G = g.n_heads / g.n_kv_heads;
+    const int64_t rows = (int64_t)std::max(g.max_new, 1) * G, blocks = ((int64_t)g.cap + 31) / 32;
+    p.few = rows <= 32;
     p.rt = rows <= 16 ? 1 : 2;
-    const int per = 16 * p.rt * (p.split_waves ? 1 : 4);
-    p.tiles = (rows + per - 1) / per;
-    // One round of the workgroups that the CUs hold at once (a second, started round costs a whole one: 130000 tokens of
-    // 8 heads at 4 bits, 96 splits 38 us, 128 splits 47 us); two splits where the sequences alone come near a round,
-    // against their different lengths.  At least 8 blocks of 32 keys each.
-    const int64_t slots = (int64_t)CUS * (p.split_waves && p.rt == 1 && dtype == BF16 ? 3 : 2);
-    const int64_t base = (int64_t)g.n_seq * g.n_kv_heads * p.tiles, blocks = ((int64_t)g.cap + 31) / 32;
-    const int64_t want = base >= 2 * slots ? 1 : base > slots / 2 ? 2 : slots / base, most = std::max<int64_t>(1, blocks / 8);
-    p.n_split = (int)std::min<int64_t>(std::min(want, most), MOST_SPLITS);
+    p.rows = p.few ? 16 * p.rt : 128;
+    const int64_t pairs = (int64_t)g.n_seq * g.n_kv_heads, tiles = (rows + p.rows - 1) / p.rows;
+    // Equal shares cost the scan and the join's launch; not where a (sequence, head) is short, nor where there are
+    // too many sequences to scan (and so enough workgroups).  A head's blocks of all sequences fit 32 bits, whatever
+    // the device finds (the tiles of all rows, and a ragged one per sequence).
+    p.scan = blocks >= WHOLE && g.n_seq <= SCAN_SEQS && ((int64_t)g.M * G / p.rows + g.n_seq) * blocks < INT32_MAX;
+    p.many_pieces = false;
+    p.groups = (int)pairs;
+    if (!p.scan) return p;
+    // one round of the workgroups that the CUs hold at once; fewer where the shares would be short
+    const int64_t slots = (int64_t)CUS * (p.few && p.rt == 1 && dtype == BF16 ? 3 : 2);
+    p.groups = (int)std::min(slots, std::max<int64_t>(1, pairs * tiles * blocks / SHARE));
+    if (p.groups > 8) p.groups &= ~7;
+    p.many_pieces = p.groups > 8 * pairs * tiles;
     return p;
 }
 
-template <int DT, int DH, typename K, typename... A>
-hipError_t run_attn(K kernel, size_t lds, dim3 grid, const CacheArgs &g, const Plan &p, const void *y, int64_t ldy, void *a,
-                    float *part, hipStream_t st, A... more) {
+template <int DT, int DH, int ROWS, typename K>
+hipError_t run_attn(K kernel, size_t lds, const CacheArgs &g, const Plan &p, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
     hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    kernel<<<grid, 256, lds, st>>>(g, y, ldy, a, part, p.n_split, more...);
+    Piece *pieces = static_cast<Piece *>(ws);
+    float *parts = reinterpret_cast<float *>(pieces + 2 * p.groups);
+    kernel<<<dim3(p.groups), 256, lds, st>>>(g, y, ldy, a, parts, pieces);
     e = hipGetLastError();
-    if (e != hipSuccess || p.n_split == 1) return e;
-    const int64_t items = (int64_t)std::max(g.max_new, 1) * g.n_heads;
-    const auto join = p.n_split <= 8 ? attn_join_kernel<DT, DH, 64> : attn_join_kernel<DT, DH, 256>;
-    const int64_t rows = p.n_split <= 8 ? 4 : 1;
-    join<<<dim3(g.n_seq, (unsigned)std::min<int64_t>((items + rows - 1) / rows, 65535)), 256, 0, st>>>(g, part, a, p.n_split);
+    if (e != hipSuccess || !p.scan || p.groups == 1) return e;
+    // the rows that the host expects (others in turn): one workgroup each where a tile has many pieces, else one for
+    // what its lanes take at once
+    const int rows = (int)std::min<int64_t>(ROWS, (int64_t)std::max(g.max_new, 1) * (g.n_heads / g.n_kv_heads));
+    const int at_once = p.many_pieces ? 1 : 4 * (64 / (DH / 4)) * 2;
+    attn_join_kernel<DT, DH, ROWS><<<dim3(p.groups - 1, (rows + at_once - 1) / at_once), 256, 0, st>>>(g, parts, pieces, p.groups, a);
     return hipGetLastError();
 }
 
 template <int DT, int DH, int BITS>
 hipError_t run_plan(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
     const Plan p = plan_of(DT, g);
-    float *part = static_cast<float *>(ws);
-    const int64_t items = (int64_t)g.n_seq * g.n_kv_heads * p.n_split;
-    if (!p.split_waves) {
-        const int64_t eights = (items + 7) / 8 * 8;
-        const int tiles = (int)std::max<int64_t>(1, std::min(p.tiles, MOST_GROUPS / eights));
-        return run_attn<DT, DH>(attn_many_kernel<DT, DH, BITS>, ManyCfg<DT, DH, BITS>::LDS, dim3((unsigned)(eights * tiles)), g, p,
-                                y, ldy, a, part, st, tiles);
-    }
-    constexpr int OCC1 = DT == BF16 ? 3 : 2, OCC2 = 2;
-    const dim3 grid((unsigned)items, (unsigned)p.tiles);
-    return p.rt == 1 ? run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 1, OCC1>, FewCfg<DT, DH, BITS, 1>::LDS, grid, g, p, y, ldy, a, part, st)
-                     : run_attn<DT, DH>(attn_few_kernel<DT, DH, BITS, 2, OCC2>, FewCfg<DT, DH, BITS, 2>::LDS, grid, g, p, y, ldy, a, part, st);
+    auto run = [&](auto scan) -> hipError_t {
+        constexpr bool SCAN = decltype(scan)::value;
+        constexpr int OCC1 = DT == BF16 ? 3 : 2, OCC2 = 2;
+        if (!p.few)
+            return run_attn<DT, DH, 128>(attn_many_kernel<DT, DH, BITS, SCAN>, ManyCfg<DT, DH, BITS>::LDS, g, p, y, ldy, a, ws, st);
+        return p.rt == 1 ? run_attn<DT, DH, 16>(attn_few_kernel<DT, DH, BITS, 1, OCC1, SCAN>, FewCfg<DT, DH, BITS, 1>::LDS, g, p, y, ldy, a, ws, st)
+                         : run_attn<DT, DH, 32>(attn_few_kernel<DT, DH, BITS, 2, OCC2, SCAN>, FewCfg<DT, DH, BITS, 2>::LDS, g, p, y, ldy, a, ws, st);
+    };
+    return p.scan ? run(std::true_type()) : run(std::false_type());
 }
 template <int DT, int DH>
 hipError_t run_bits(const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {
@@ -898,7 +1066,7 @@ hipError_t run_dh(const CacheArgs &g, const void *y, int64_t ldy, void *a, void 
 
 size_t attn_cache_ws_bytes(int dtype, const CacheArgs &g) {
     const Plan p = plan_of(dtype, g);
-    return p.n_split == 1 ? 0 : (size_t)g.M * g.n_heads * p.n_split * (g.head_dim + 4) * sizeof(float);
+    return p.scan ? (size_t)2 * p.groups * (sizeof(Piece) + (size_t)p.rows * (g.head_dim + 4) * sizeof(float)) : 0;
 }
 
 hipError_t launch_attn_cache(int dtype, const CacheArgs &g, const void *y, int64_t ldy, void *a, void *ws, hipStream_t st) {

@@ -90,7 +90,9 @@ def test_attention_workspace():
     assert size(_prob(), _cache(**none), _rows(pages=None, past=None, start=None)) == 0
     p, r = _prob(seq_len=1), _rows(n_seq=1, max_pages=512, max_new=1)
     n = size(p, _cache(page_size=256), r)
-    assert n > 0 and n % ((64 + 4) * 4 * 4) == 0           # a share per (row, head, split): O, m, l
+    assert n >= 2 * 2 * 16 * (64 + 4) * 4                  # two pieces of 16 rows for each share: O, m, l
+    # it does not grow with the batch's rows
+    assert size(_prob(seq_len=1 << 20), _cache(page_size=256), r) == n
     assert size(_prob(head_dim=32), _cache(), r) == size(p, _cache(bits=5), r) == ctypes.c_size_t(-1).value
     attn = _calls(p, _cache(page_size=256), r, ws_bytes=n - 1)["attn"]
     assert attn() == jab.JAB_E_WORKSPACE

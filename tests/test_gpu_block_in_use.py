@@ -320,10 +320,10 @@ def test_cache_bad_tables():
 
 
 # ------------------------------------------------------------------ attention
-def _values(su, i, length):
-    """keys and values [2][length][hkv][dh] of sequence i in fp64, from the cache's codes"""
+def _values(su, host, i, length):
+    """keys and values [2][length][hkv][dh] of sequence i in fp64, from the cache's codes (host: its tensors)"""
     pages, out = su.pages.cpu().numpy(), []
-    kc, vc, ks, vs, kz, vz = [None if t is None else t.cpu().numpy() for t in su.cache.tensors]
+    kc, vc, ks, vs, kz, vz = host
     for c, s, z, tr in ((kc, ks, kz, False), (vc, vs, vz, True)):
         rows = []
         for col in range((length + su.page - 1) // su.page):
@@ -338,9 +338,9 @@ def _values(su, i, length):
     return np.stack(out)
 
 
-def _largest_scale(su, i, length):
+def _largest_scale(su, host, i, length):
     """the largest value scale of sequence i per query head"""
-    s = su.cache.tensors[3][su.pages[i, : (length + su.page - 1) // su.page].long()].double().cpu().numpy()
+    s = host[3][su.pages[i, : (length + su.page - 1) // su.page].cpu().numpy()].astype(np.float64)
     s = s.transpose(1, 0, 2).reshape(su.hkv, -1)[:, :length].max(1)
     return np.repeat(s, su.hq // su.hkv)
 
@@ -360,11 +360,14 @@ def _attend(su, y):
     u = 2.0 ** (-11 if su.dtype == torch.bfloat16 else -22)
     want, tol = np.zeros((su.M, su.hq * su.dh)), np.zeros((su.M, su.hq * su.dh))
     row = 0
+    host = [None if t is None else t.cpu().numpy() for t in su.cache.tensors]
     for i, (a, n) in enumerate(su.seqs):
+        if n == 0:
+            continue
         q = yn[row:row + n, : su.hq * su.dh].reshape(n, su.hq, su.dh)
         if su.rope:
             q = _turned(q, np.arange(a, a + n), su.rope)
-        k, v = _values(su, i, a + n)
+        k, v = _values(su, host, i, a + n)
         k, v = np.repeat(k, su.hq // su.hkv, 1), np.repeat(v, su.hq // su.hkv, 1)
         z = np.einsum("nhd,thd->hnt", q, k) / math.sqrt(su.dh)
         S = np.einsum("nhd,thd->hnt", np.abs(q), np.abs(k)) / math.sqrt(su.dh)
@@ -380,7 +383,7 @@ def _attend(su, y):
         A = np.einsum("hnt,thd->nhd", w, np.abs(v))
         want[row:row + n] = o.reshape(n, -1)
         t = A * rel.T[..., None] + np.abs(o) * torch.finfo(su.dtype).eps / 2 + 2.0 ** -149
-        t = t + ((a + n) * 255 * 2.0 ** -30 * _largest_scale(su, i, a + n))[None, :, None]
+        t = t + ((a + n) * 255 * 2.0 ** -30 * _largest_scale(su, host, i, a + n))[None, :, None]
         if su.dtype == torch.float16:
             t = t + 2.0 ** -25                             # half a step of its subnormals
         tol[row:row + n] = t.reshape(n, -1)
@@ -436,6 +439,38 @@ def test_attention_with_a_split_key_axis(dtype, bits, seqs):
     su = Setup(dtype, seqs, 8, 2, 128 if bits == 8 else 64, bits, rope=10000.0, page=64)
     assert jab.attn_cache_workspace(su.p, su.cache, su.rows).numel() > 0
     su.history()
+    y = su.y(su.M, 3.0)
+    jab.cache_write(su.p, su.cache, su.rows, y)
+    _check_attention(su, y)
+
+
+@pytest.mark.parametrize("dtype,bits,dh,seqs", [
+    # one sequence far longer than the others, some without new tokens, cuts inside and between heads
+    ("bf16", 8, 128, [(3, 1), (20000, 1), (0, 0), (900, 2), (40, 1), (0, 0), (2500, 1), (7, 3)]),
+    ("f32", 4, 16, [(0, 0), (12000, 1), (5, 1), (5, 0), (700, 1), (0, 0)]),
+    ("f16", 8, 64, [(100, 6)] * 30 + [(4000, 8)] + [(0, 1)] * 40),
+    # tiles of many rows cut between workgroups
+    ("bf16", 8, 64, [(3000, 150), (0, 0), (10, 70), (0, 400), (1500, 1)]),
+    ("f32", 8, 16, [(0, 700), (2000, 40)]),
+])
+def test_attention_of_uneven_sequences(dtype, bits, dh, seqs):
+    su = Setup(dtype, seqs, 8, 2, dh, bits, rope=10000.0, page=64, spare_rows=1)
+    su.history()
+    y = su.y(su.M, 3.0)
+    jab.cache_write(su.p, su.cache, su.rows, y)
+    _check_attention(su, y)
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_attention_of_many_sequences(new):
+    """More sequences than a workgroup scans: one workgroup per (sequence, head)."""
+    rng = np.random.default_rng(5)
+    seqs = [(int(a), int(n)) for a, n in zip(rng.integers(0, 60, 600), rng.integers(0, new + 1, 600))]
+    su = Setup("bf16", seqs, 8, 2, 16, page=32)
+    y0 = su.y(sum(a for a, _ in seqs))                     # all the histories in one call
+    p = _problem("bf16", y0.shape[1], 64, 8, 2, 16)
+    start = torch.tensor(np.cumsum([0] + [a for a, _ in seqs]), dtype=torch.int32, device="cuda")
+    jab.cache_write(p, su.cache, jab.CacheRows(su.pages, torch.zeros_like(su.past), start, 60), y0)
     y = su.y(su.M, 3.0)
     jab.cache_write(su.p, su.cache, su.rows, y)
     _check_attention(su, y)
