@@ -32,7 +32,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LAZY = 8.f;             // log2 of what a score may exceed the reference by
 constexpr int WUP = 6;                  // log2 of the weights' extra scale: p sv <= 2^(8 + 6) in fp16
-constexpr int EMIN = -125;
+constexpr int EMIN = -119;              // 2^(WUP - EMIN) is finite
 constexpr int NOWHERE = INT32_MAX - 63; // a key past every position
 
 // two codes of a word as fp16 integers, 1024 + code: bytes 0, 1 (hi false) or 2, 3
@@ -148,7 +148,7 @@ struct Wave {
             for (int t = 0; t < L::NT; ++t) o[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // S^T of a block, kop(t, ks) the key operands
+    // S^T of a block, kop(t, ks) the key operands (few at a time in registers)
     template <typename F>
     __device__ inline void scores(f32x4 (&st)[RT][2], F &&kop) {
 #pragma unroll
@@ -166,12 +166,14 @@ struct Wave {
             }
         }
     }
-    // the scores in key units: times the keys' scales, -inf where not seen (key0: this lane's first key)
-    __device__ inline void scale(f32x4 (&st)[RT][2], const f32x4 (&ks)[2], bool edge, int key0) {
+    // the scores in key units: times the keys' scales; -inf where not seen (key0: this lane's first key)
+    __device__ inline void scale(f32x4 (&st)[RT][2], const f32x4 (&ks)[2]) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int i = 0; i < 8; ++i) st[rt][i >> 2][i & 3] *= ks[i >> 2][i & 3];
+    }
+    __device__ inline void mask(f32x4 (&st)[RT][2], bool edge, int key0) {
         if (edge) {
             asm volatile("");                              // a branch, so that other blocks pay nothing for the masks
 #pragma unroll
@@ -181,78 +183,86 @@ struct Wave {
                     st[rt][i >> 2][i & 3] = key0 + i <= lim[rt] ? st[rt][i >> 2][i & 3] : -__builtin_inff();
         }
     }
-    // weights of a block's scores; moves the references where a score or a value scale asks for it
-    __device__ inline void weights(const f32x4 (&st)[RT][2], const f32x4 (&vsc)[2], bool edge, int key0, f16x8 (&pw)[RT][NP]) {
-        float vs[8], big = 0.f;
+    // A block's value scales.  In a block that not every row sees whole, what was never written (or has no page) may be
+    // anything and counts 0; and a value that is NaN goes over to the scores of the rows that see it, since its
+    // product with the weight 0 of the others would be NaN too.
+    __device__ inline void value_scales(f32x4 (&st)[RT][2], const f32x4 (&vsc)[2], bool edge, int key0, float (&vs)[8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) vs[i] = vsc[i >> 2][i & 3];
-        if (edge) {                                        // what was never written may be anything
+        if (edge) {
             asm volatile("");
 #pragma unroll
-            for (int i = 0; i < 8; ++i) vs[i] = key0 + i <= hi_lim ? vs[i] : 0.f;
+            for (int i = 0; i < 8; ++i) {
+                const bool in = key0 + i <= hi_lim, fine = fabsf(vs[i]) < __builtin_inff();
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float t = st[rt][i >> 2][i & 3];
+                    st[rt][i >> 2][i & 3] = fine || t == -__builtin_inff() ? t : __builtin_nanf("");
+                }
+                vs[i] = in && fine ? vs[i] : 0.f;
+            }
         }
+    }
+    // the references moved where a block's scores or value scales ask for it, with every sum so far
+    __device__ inline void move(const f32x4 (&st)[RT][2], const float (&vs)[8]) {
+        float big = 0.f, top[RT];
 #pragma unroll
         for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(vs[i]));
-        float top[RT];
-        bool move = big > Rmax;
+        bool any = big > Rmax;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             top[rt] = st[rt][0][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) top[rt] = fmaxf(top[rt], st[rt][i >> 2][i & 3]);
-            move |= top[rt] * fs[rt] > m[rt] + LAZY;
+            any |= top[rt] * fs[rt] > m[rt] + LAZY;
         }
-        if (__builtin_amdgcn_ballot_w64(move)) {
-            big = fmaxf(big, __shfl_xor(big, 16, 64));
-            big = fmaxf(big, __shfl_xor(big, 32, 64));
-            int En = E;
-            if (big > Rmax) En = min((int)(__builtin_bit_cast(uint32_t, big) >> 23) - 127 + 1, 125);
-            En = __builtin_amdgcn_readfirstlane(En);
-            const float down = pow2i(max(E - En, -126));
-            E = En;
-            Rmax = pow2i(E);
-            rinv = pow2i(-E);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float t = top[rt];
-                t = fmaxf(t, __shfl_xor(t, 16, 64));
-                t = fmaxf(t, __shfl_xor(t, 32, 64));
-                const float mn = fmaxf(m[rt], t * fs[rt]);
-                const float al = mn == m[rt] ? 1.f : exp2f(m[rt] - mn);
-                m[rt] = mn;
-                nm[rt] = mn == -__builtin_inff() ? 0.f : -mn;
-                l[rt] *= al;
-                const float f = al * down;
-#pragma unroll
-                for (int t2 = 0; t2 < L::NT; ++t2)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[rt][t2][i] *= f;
-            }
-        }
-        const float up = rinv * (float)(1 << WUP);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) vs[i] *= up;
+        if (!__builtin_amdgcn_ballot_w64(any)) return;
+        big = fmaxf(big, __shfl_xor(big, 16, 64));
+        big = fmaxf(big, __shfl_xor(big, 32, 64));
+        int En = E;
+        if (big > Rmax) En = min((int)(__builtin_bit_cast(uint32_t, big) >> 23) - 127 + 1, 125);
+        En = __builtin_amdgcn_readfirstlane(En);
+        const float down = pow2i(max(E - En, -126));
+        E = En;
+        Rmax = pow2i(E);
+        rinv = pow2i(-E);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            float w[8];
+            float t = top[rt];
+            t = fmaxf(t, __shfl_xor(t, 16, 64));
+            t = fmaxf(t, __shfl_xor(t, 32, 64));
+            const float mn = fmaxf(m[rt], t * fs[rt]);
+            const float al = mn == m[rt] ? 1.f : exp2f(m[rt] - mn);
+            m[rt] = mn;
+            nm[rt] = mn == -__builtin_inff() ? 0.f : -mn;
+            l[rt] *= al;
+            const float f = al * down;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][i >> 2][i & 3], fs[rt], nm[rt]));
-                l[rt] += p;
-                w[i] = p * vs[i];
+            for (int t2 = 0; t2 < L::NT; ++t2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rt][t2][i] *= f;
+        }
+    }
+    // the weights of two scores of a lane: piece j = 4 rt + k, keys 2 k and 2 k + 1; vs: the value scales times up()
+    __device__ inline float up() const { return rinv * (float)(1 << WUP); }
+    __device__ inline void weight2(int j, const f32x4 (&st)[RT][2], const float (&vs)[8], f16x8 (&pw)[RT][NP]) {
+        const int rt = j >> 2, i = 2 * (j & 3);
+        float w[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][i >> 2][(i & 3) + e], fs[rt], nm[rt]));
+            l[rt] += p;
+            w[e] = p * vs[i + e];
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const f16x2 hw = __builtin_convertvector(f32x2_t{w[0], w[1]}, f16x2);
+            pw[rt][p][i] = hw[0];
+            pw[rt][p][i + 1] = hw[1];
+            if (p + 1 < NP) {
+                w[0] -= (float)hw[0];
+                w[1] -= (float)hw[1];
             }
-#pragma unroll
-            for (int p = 0; p < NP; ++p)
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const f16x2 hw = __builtin_convertvector(f32x2_t{w[i], w[i + 1]}, f16x2);
-                    pw[rt][p][i] = hw[0];
-                    pw[rt][p][i + 1] = hw[1];
-                    if (p + 1 < NP) {
-                        w[i] -= (float)hw[0];
-                        w[i + 1] -= (float)hw[1];
-                    }
-                }
         }
     }
     // O^T += V^T P^T, vop(t) the value operands
@@ -671,11 +681,19 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
 #pragma unroll
                 for (int t = 0; t < 2; ++t) zk[t][0] = zk[t][1] = zk[t][2] = zk[t][3] = both(kz[t]);
                 w.scores(st, [&](int t, int step) { return L::kop(k[t], step, grp, zk[t]); });
-                w.scale(st, ks, edge, key0);
+                w.scale(st, ks);
+                w.mask(st, edge, key0);
                 __builtin_amdgcn_sched_barrier(0);
                 load_k(max(next, (int64_t)0));             // after the last block: page 0, not used
                 __builtin_amdgcn_sched_barrier(0);
-                w.weights(st, vs, edge, key0, pw);
+                float vsc[8];
+                w.value_scales(st, vs, edge, key0, vsc);
+                w.move(st, vsc);
+                const float up = w.up();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) vsc[i] *= up;
+#pragma unroll
+                for (int j = 0; j < 4 * RT; ++j) w.weight2(j, st, vsc, pw);
                 f16x2 zv[4] = {biased(vz[0], false), biased(vz[0], true), biased(vz[1], false), biased(vz[1], true)};
                 if (!asym) zv[0] = zv[1] = zv[2] = zv[3] = both(QMID);
                 w.values(pw, [&](int t) { return L::vop(v, t, l16, zv); });
@@ -726,19 +744,19 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
 }
 
 // ---------------------------------------------------------------- many rows
-// Each wave has 32 rows of its own; the workgroup turns two blocks of 32 tokens at a time into operands in LDS,
-// which its four waves share (waves 0, 1 the keys, 2, 3 the values of the two blocks; an operand is 64 lanes x 16
-// bytes, written and read without conflicts).  The next two blocks' bytes are in flight meanwhile; two stages, one
-// barrier per stage.
+// Each wave has 32 rows of its own; the workgroup turns a block of 32 tokens at a time into operands in LDS, which its
+// four waves share (waves 0, 1 the two key tiles, 2, 3 half of the values each; an operand is 64 lanes x 16 bytes, written
+// and read without conflicts).  Three blocks in a ring, one barrier per block; bytes are asked for two blocks before
+// they are turned, page numbers before that.  The scores of the next block are formed beside the weights of this one,
+// and the next but one is turned beside this one's second product, so that matrix and vector instructions of one wave overlap.
 template <int DT, int DH, int BITS>
 struct ManyCfg {
     typedef Lay<DH, BITS> L;
     static constexpr int RT = 2, ROWS = 128;
     static constexpr int KOPS = 2 * L::KS, OPS = KOPS + L::NT;                   // operands of a block
     static constexpr int BLOCK = OPS * 1024 + 256;                               // and its 32 + 32 scales
-    static constexpr size_t STAGE = 2 * BLOCK;
     static constexpr size_t Q_LDS = (size_t)Wave<DT, DH, BITS, RT>::NP * 4 * 16 * QP<DH> * 2;
-    static constexpr size_t LDS = 2 * STAGE > Q_LDS ? 2 * STAGE : Q_LDS;
+    static constexpr size_t LDS = 3 * BLOCK > Q_LDS ? 3 * BLOCK : Q_LDS;
 };
 
 template <int DT, int DH, int BITS, bool SCAN>
@@ -749,6 +767,8 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
     typedef Wave<DT, DH, BITS, S::RT> W;
     typedef Lay<DH, BITS> L;
     constexpr int QMID = (1 << (BITS - 1)) - 1, RT = S::RT;
+    constexpr int VH = L::VU < 2 ? 1 : L::VU / 2;          // value units of a wave
+    constexpr int RU = VH;                                 // units of a wave
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float rowf[64];
     const int lane = threadIdx.x & 63;
@@ -756,9 +776,18 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
     const int l16 = lane & 15, grp = lane >> 4;
     const int G = g.n_heads / g.n_kv_heads;
     const bool asym = g.k_zero != nullptr;
-    const int kind = wave >> 1, mine = wave & 1;           // what this wave prepares: keys or values, of which block
-    const uint8_t *code_base = kind ? g.v : g.k, *zero_base = kind ? g.v_zero : g.k_zero;
+    const int kind = wave >> 1, mine = wave & 1;           // what this wave turns: keys or values, which half
+    // (the symmetric grid has no zero-points: bytes that exist are read in their place, and not used)
+    const uint8_t *code_base = kind ? g.v : g.k, *zero_base = !asym ? code_base : kind ? g.v_zero : g.k_zero;
     const uint8_t *scale_base = reinterpret_cast<const uint8_t *>(kind ? g.v_scale : g.k_scale);
+    // a lane's byte offsets inside a block
+    const uint32_t off = kind ? L::vrow(0, l16) * 32 + 8 * grp + (L::VU < 2 ? 0 : mine * VH * 512)
+                              : L::key(mine, l16) * L::DHB + L::kbyte(0, grp);
+    const uint32_t zoff = kind ? 8 * grp : L::key(mine, l16) & ~3u, zoff2 = kind ? zoff + 4 : zoff;
+    const int zsh = kind ? 0 : 8 * (L::key(mine, l16) & 3);
+    static_assert(DH < 64 || L::KU == VH, "keys and values alike");
+    const int first = kind ? S::KOPS + (DH < 64 ? 0 : mine * VH) : mine * L::KS, high = kind ? L::NT / 2 : L::KU;
+    const int nib = kind ? (l16 >> 3) * 4 : (grp & 1) * 4;
     const int share = SCAN ? share_of(blockIdx.x, gridDim.x) : blockIdx.x;
     Share<S::ROWS, SCAN> sh;
     sh.find(g, G, share, gridDim.x, lane);
@@ -777,6 +806,69 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
         }
         sh.left -= end - b0;
         sh.advance(g, G);
+
+        // ---- this wave's share of a block's bytes
+        struct Bytes {
+            u32x2 u[RU], z;
+            float sc;
+        } raw;
+        auto page_at = [&](int b) {
+            const int p = page_of(g, s, min(b, end - 1) * 32);
+            return b < end ? p : -1;
+        };
+        auto load = [&](Bytes &r, int b, int page) {       // (no page, or past the end: page 0, not used)
+            const int64_t at = (((int64_t)max(page, 0) * g.n_kv_heads + h) << g.page_shift) +
+                               ((b * 32) & ((1 << g.page_shift) - 1));
+            const uint8_t *codes = code_base + at * L::DHB;
+#pragma unroll
+            for (int u = 0; u < RU; ++u) {
+                const uint32_t ko = L::kbyte(u, 0), vo = 512 * u;
+                r.u[u] = ldu<u32x2>(codes, off + (kind ? vo : ko));
+            }
+            r.z[0] = ldu<uint32_t>(zero_base + at, zoff);
+            r.z[1] = ldu<uint32_t>(zero_base + at, zoff2);
+            r.sc = ldu<float>(scale_base + 4 * at, 4 * (lane & 31));
+        };
+        // the operands of this wave's bytes, keys and values alike (no branch: the loop's instructions are one
+        // block to schedule): unit u is operand first + u, at 4 bits its high halves operand first + u + high
+        f16x2 z[4];
+        auto turn_zero = [&](const Bytes &r) {
+            const uint32_t kz = ((r.z[0] >> zsh) & 255u) * 0x01010101u, mid = QMID * 0x01010101u;
+            const uint32_t z0 = !asym ? mid : kind ? r.z[0] : kz, z1 = !asym ? mid : kind ? r.z[1] : kz;
+            z[0] = biased(z0, false);
+            z[1] = biased(z0, true);
+            z[2] = biased(z1, false);
+            z[3] = biased(z1, true);
+        };
+        auto turn_unit = [&](const Bytes &r, int u, unsigned char *blk) {
+            unsigned char *dst = blk + first * 1024 + lane * 16;
+            const uint32_t w0 = r.u[u][0], w1 = r.u[u][1];
+            if constexpr (BITS == 8) {
+                *reinterpret_cast<f16x8 *>(dst + u * 1024) = codes8(w0, w1, z);
+            } else if constexpr (DH < 64) {
+                *reinterpret_cast<f16x8 *>(dst) = codes8((w0 >> nib) & 0x0F0F0F0Fu, (w1 >> nib) & 0x0F0F0F0Fu, z);
+            } else {
+                *reinterpret_cast<f16x8 *>(dst + u * 1024) = codes8(w0 & 0x0F0F0F0Fu, w1 & 0x0F0F0F0Fu, z);
+                *reinterpret_cast<f16x8 *>(dst + (u + high) * 1024) =
+                    codes8((w0 >> 4) & 0x0F0F0F0Fu, (w1 >> 4) & 0x0F0F0F0Fu, z);
+            }
+        };
+        auto turn_scales = [&](const Bytes &r, unsigned char *blk) {             // (by both waves of a kind: the same)
+            *reinterpret_cast<float *>(blk + S::OPS * 1024 + kind * 128 + (lane & 31) * 4) = r.sc;
+        };
+        auto turn_block = [&](const Bytes &r, unsigned char *blk) {
+            turn_zero(r);
+#pragma unroll
+            for (int u = 0; u < RU; ++u) turn_unit(r, u, blk);
+            turn_scales(r, blk);
+        };
+        // pages of blocks b .. b + 5 as b advances (scalar loads); bytes of b + 2 and b + 3 in registers
+        int pg[5];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) pg[i] = page_at(b0 + i);
+        load(raw, b0, pg[0]);
+
+        // ---- queries
         W w;
         _Float16 *ql = reinterpret_cast<_Float16 *>(smem) + wave * 16 * QP<DH>;
         constexpr int QSTRIDE = 4 * 16 * QP<DH>;
@@ -792,87 +884,107 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
                 for (int ks = 0; ks < L::KS; ++ks)
                     w.qf[rt][p][ks] = *reinterpret_cast<const f16x8 *>(ql + p * QSTRIDE + l16 * QP<DH> + L::dim(ks, grp));
         }
-        __syncthreads();                                   // the stages lie over the queries
+        __syncthreads();                                   // the ring lies over the queries
         w.limits(g, sr, G, row0, n_rows, l16);
         w.start();
 
-        u32x2 raw[2 * L::KU > L::VU ? 2 * L::KU : L::VU], vz = {0, 0};
-        int kz[2] = {QMID, QMID};
-        float sc = 0.f;
-        const uint32_t zoff = L::key(0, l16), koff = zoff * L::DHB + L::kbyte(0, grp), voff = L::vrow(0, l16) * 32 + 8 * grp;
-        auto page_at = [&](int b) { return b < end ? page_of(g, s, b * 32) : -1; };
-        auto load = [&](int b, int page) {                 // this wave's share of a stage: of block b, in that page
-            const int64_t at = (((int64_t)max(page, 0) * g.n_kv_heads + h) << g.page_shift) +
-                               ((b * 32) & ((1 << g.page_shift) - 1));
-            const uint8_t *codes = code_base + at * L::DHB;
-            if (kind == 0) {
+        int slot = 0;                                      // byte offset of block b in the ring
+        auto next = [&](int at) { return at == 2 * S::BLOCK ? 0 : at + S::BLOCK; };
+        turn_block(raw, smem);
+        load(raw, b0 + 1, pg[1]);
+        turn_block(raw, smem + S::BLOCK);
+        load(raw, b0 + 2, pg[2]);
+        __syncthreads();
+
+        // block b's scores (scaled and masked) and value scales, as the loop's body for b wants them
+        constexpr int NQ = 2 * L::KS;
+        f32x4 st[RT][2];
+        float vs[8];
+        auto operand = [&](const unsigned char *blk, int i) { return *reinterpret_cast<const f16x8 *>(blk + i * 1024 + lane * 16); };
+        auto product = [&](f32x4 (&to)[RT][2], int i, f16x8 k) {       // key operand i
+            const int t = i / L::KS, ks = i % L::KS;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
+            for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                    for (int u = 0; u < L::KU; ++u) raw[t * L::KU + u] = ldu<u32x2>(codes, koff + 4 * t * L::DHB + L::kbyte(u, 0));
-                    if (asym) kz[t] = ldu<uint8_t>(zero_base + at, zoff + 4 * t);
-                }
-            } else {
-#pragma unroll
-                for (int u = 0; u < L::VU; ++u) raw[u] = ldu<u32x2>(codes, voff + 512 * u);
-                if (asym) vz = ldu<u32x2>(zero_base + at, 8 * grp);
-            }
-            sc = ldu<float>(scale_base + 4 * at, 4 * (lane & 31));
+                for (int p = 0; p < W::NP; ++p)
+                    to[rt][t] = mma16(k, w.qf[rt][p][ks], ks == 0 && p == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : to[rt][t]);
         };
-        auto prepare = [&](int buf) {                      // into stage buf
-            unsigned char *blk = smem + buf * S::STAGE + mine * S::BLOCK;
-            if (kind == 0) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const f16x2 z1 = both(kz[t]), z[4] = {z1, z1, z1, z1};
-                    u32x2 k[L::KU];
-#pragma unroll
-                    for (int u = 0; u < L::KU; ++u) k[u] = raw[t * L::KU + u];
-#pragma unroll
-                    for (int ks = 0; ks < L::KS; ++ks)
-                        *reinterpret_cast<f16x8 *>(blk + (t * L::KS + ks) * 1024 + lane * 16) = L::kop(k, ks, grp, z);
-                }
-            } else {
-                f16x2 z[4] = {biased(vz[0], false), biased(vz[0], true), biased(vz[1], false), biased(vz[1], true)};
-                if (!asym) z[0] = z[1] = z[2] = z[3] = both(QMID);
-                u32x2 v[L::VU];
-#pragma unroll
-                for (int u = 0; u < L::VU; ++u) v[u] = raw[u];
-#pragma unroll
-                for (int t = 0; t < L::NT; ++t)
-                    *reinterpret_cast<f16x8 *>(blk + (S::KOPS + t) * 1024 + lane * 16) = L::vop(v, t, l16, z);
-            }
-            if (lane < 32) *reinterpret_cast<float *>(blk + S::OPS * 1024 + kind * 128 + lane * 4) = sc;
+        auto mask = [&](f32x4 (&to)[RT][2], int b, int page) {
+            const bool edge = page < 0 || b * 32 + 31 > w.lo_lim;
+            const int key0 = page < 0 ? NOWHERE : b * 32 + 8 * grp;
+            w.mask(to, edge, key0);
+            const f32x4 v[2] = {f32x4{vs[0], vs[1], vs[2], vs[3]}, f32x4{vs[4], vs[5], vs[6], vs[7]}};
+            w.value_scales(to, v, edge, key0, vs);
         };
-        // page numbers (scalar loads) two stages ahead, bytes one stage ahead
-        int buf = 0, pg[2] = {page_at(b0), page_at(b0 + 1)}, pn[2] = {page_at(b0 + 2), page_at(b0 + 3)};
-        if (b0 < end) load(b0 + mine, mine ? pg[1] : pg[0]);
-        for (int b = b0; b < end; b += 2) {
-            const int pf[2] = {page_at(b + 4), page_at(b + 5)};
-            prepare(buf);
-            if (b + 2 < end) load(b + 2 + mine, mine ? pn[1] : pn[0]);
+        auto scales = [&](const unsigned char *blk, int i) {           // two times 16 bytes of key, then of value scales
+            return *reinterpret_cast<const f32x4 *>(blk + S::OPS * 1024 + (i >> 1) * 128 + 32 * grp + 16 * (i & 1));
+        };
+        {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) product(st, i, operand(smem, i));
+            const f32x4 ks[2] = {scales(smem, 0), scales(smem, 1)};
+            w.scale(st, ks);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vs[i] = scales(smem, 2 + (i >> 2))[i & 3];
+            mask(st, b0, pg[0]);
+        }
+        for (int b = b0; b < end; ++b) {
+            const unsigned char *cur = smem + slot, *nxt = smem + next(slot);
+            unsigned char *fill = smem + next(next(slot));
+            const int ahead = page_at(b + 5);
+            f16x8 op[NQ > L::NT ? NQ : L::NT];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) op[i] = operand(nxt, i);
+            w.move(st, vs);
+            const float up = w.up();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vs[i] *= up;
+            __builtin_amdgcn_sched_barrier(0);
+            // the next block's scores (past the end: of what the ring holds, not used) beside this block's weights
+            f32x4 sn[RT][2];
+            f16x8 pw[RT][W::NP], vo[L::NT];
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                if (i + 2 < NQ) op[i + 2] = operand(nxt, i + 2);
+                else if (i + 2 - NQ < L::NT) vo[i + 2 - NQ] = operand(cur, S::KOPS + i + 2 - NQ);
+                product(sn, i, op[i]);
+#pragma unroll
+                for (int j = i * 4 * RT / NQ; j < (i + 1) * 4 * RT / NQ; ++j) w.weight2(j, st, vs, pw);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // this block's second product beside the turning of the next but one and the next one's scales
+            f32x4 sc4[4];
+            turn_zero(raw);
+#pragma unroll
+            for (int t = 0; t < L::NT; ++t) {
+                if (t + 2 < L::NT) vo[t + 2] = operand(cur, S::KOPS + t + 2);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int p = 0; p < W::NP; ++p) w.o[rt][t] = mma16(vo[t], pw[rt][p], w.o[rt][t]);
+#pragma unroll
+                for (int u = t * RU / L::NT; u < (t + 1) * RU / L::NT; ++u) turn_unit(raw, u, fill);
+                if (t == 0)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc4[i] = scales(nxt, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            turn_scales(raw, fill);
+            load(raw, b + 3, pg[3]);
+            const f32x4 ksn[2] = {sc4[0], sc4[1]};
+            w.scale(sn, ksn);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vs[i] = sc4[2 + (i >> 2)][i & 3];
+            mask(sn, b + 1, pg[1]);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) st[rt][t] = sn[rt][t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pg[i] = pg[i + 1];
+            pg[4] = ahead;
+            slot = next(slot);
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned char *blk = smem + buf * S::STAGE + i * S::BLOCK;
-                if (pg[i] < 0 || (b + i) * 32 > w.hi_lim) continue;             // no page (or past the end), or past this wave's rows
-                const int key0 = (b + i) * 32 + 8 * grp;
-                const bool edge = (b + i) * 32 + 31 > w.lo_lim;
-                const f32x4 *scl = reinterpret_cast<const f32x4 *>(blk + S::OPS * 1024);
-                f32x4 st[RT][2];
-                f16x8 pw[RT][W::NP];
-                w.scores(st, [&](int t, int ks) { return *reinterpret_cast<const f16x8 *>(blk + (t * L::KS + ks) * 1024 + lane * 16); });
-                const f32x4 ks[2] = {scl[2 * grp], scl[2 * grp + 1]}, vs[2] = {scl[8 + 2 * grp], scl[8 + 2 * grp + 1]};
-                w.scale(st, ks, edge, key0);
-                w.weights(st, vs, edge, key0, pw);
-                w.values(pw, [&](int t) { return *reinterpret_cast<const f16x8 *>(blk + (S::KOPS + t) * 1024 + lane * 16); });
-            }
-            buf ^= 1;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                pg[i] = pn[i];
-                pn[i] = pf[i];
-            }
         }
         w.finish();
 #pragma unroll

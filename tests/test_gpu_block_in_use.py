@@ -525,16 +525,44 @@ def test_attention_rows_that_see_nothing():
     assert not bool((a[0, 30:43] == 0).all(1).any()) and bool((a[0, 43] == 9).all())
 
 
-def test_attention_nan_stays_in_its_rows():
-    su = Setup("bf16", [(0, 40), (0, 3)], 8, 2, 64, page=32, spare_rows=0)
-    y = su.y(su.M, 2.0)
-    y[0, 7, 3] = math.nan                                  # a query of head 0
-    y[0, 41, 8 * 64 + 1] = math.inf                        # a key of head 0, sequence 1: seen by its rows from there on
+@pytest.mark.parametrize("past", [40, 5000])
+def test_attention_single_tokens_without_their_first_pages(past):
+    """A decoding step whose first pages are gone sees the rest, and 0 where all are gone."""
+    su = Setup("bf16", [(past, 1), (past, 1)], 8, 2, 64, page=32, spare_rows=0)
+    su.history()
+    y = su.y(2, 2.0)
     jab.cache_write(su.p, su.cache, su.rows, y)
-    bad = jab.attn_cache(su.p, su.cache, su.rows, y)[0].reshape(43, 8, 64).isnan()
-    want = torch.zeros(43, 8, dtype=torch.bool, device="cuda")
-    want[7, 0] = True
-    want[41:, :4] = True
+    gone = past // 32                                      # the new token's own page stays
+    pages = su.pages.clone()
+    pages[0, :gone] = -1
+    pages[1] = -1
+    a = jab.attn_cache(su.p, su.cache, jab.CacheRows(pages, su.past, su.start, 1), y)[0]
+    assert bool((a[1] == 0).all())
+    # the same tokens as a short sequence of their own (no rotary embedding: positions do not matter)
+    n = past + 1 - 32 * gone
+    one = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")               # noqa: E731
+    b = jab.attn_cache(_problem("bf16", 1, 64, 8, 2, 64), su.cache,
+                       jab.CacheRows(su.pages[:1, gone:].contiguous(), one([n - 1]), one([0, 1]), 1), y[:, :1].contiguous())[0]
+    # half a step of bf16 each, and the weights' 2^-11 of sum p |v|, at most the largest |v|
+    v = jab.cache_read(_problem("bf16", n, 64, 8, 2, 64), su.cache,
+                       jab.CacheRows(su.pages[:1, gone:].contiguous(), one([0]), one([0, n]), n))[1].abs().max().item()
+    assert float((a[0] - b[0]).abs().max()) <= 2 * (2.0 ** -8 + 2.0 ** -11) * v
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("first,second", [(40, 3), (3, 2)])                          # many rows, few rows
+def test_attention_nan_stays_in_its_rows(dtype, first, second):
+    su = Setup(dtype, [(0, first), (0, second)], 8, 2, 64, page=32, spare_rows=0)
+    y = su.y(su.M, 2.0)
+    y[0, 2, 3] = math.nan                                  # a query of head 0
+    y[0, first + 1, 8 * 64 + 1] = math.inf                 # a key of head 0, sequence 1: seen by its rows from there on
+    y[0, 1, 11 * 64 + 5] = math.nan                        # a value of head 1, sequence 0
+    jab.cache_write(su.p, su.cache, su.rows, y)
+    bad = jab.attn_cache(su.p, su.cache, su.rows, y)[0].reshape(su.M, 8, 64).isnan()
+    want = torch.zeros(su.M, 8, dtype=torch.bool, device="cuda")
+    want[2, 0] = True
+    want[first + 1:, :4] = True
+    want[1:first, 4:] = True
     assert torch.equal(bad.any(-1), want) and torch.equal(bad.all(-1), want)
 
 
