@@ -398,13 +398,29 @@ def loss_bwd_kl(p: Problem, x, w, bits, scale, zero, a_ref, qk_ref, lse_ref, gsc
 
 
 # --------------------------------------------------------------------------- the block in use
-def _arg(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device=None) -> int:
-    """The address of a contiguous tensor of this dtype and shape on this device (None: the current one)."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+# A decoding step is a few microseconds on the device, so these calls keep what the host does short: the tensors'
+# dtype, shape, layout and device are checked here, everything else in the library.
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+
+
+def _here(t: torch.Tensor) -> int:
+    """The current GPU, on which the call's tensors have to be (t: one of them)."""
+    if not t.is_cuda:
+        raise JabError(JAB_E_INVALID, f"a tensor is on {t.device}, not on the current GPU")
+    return torch.cuda.current_device()
+
+
+def _stream_of(dev: int) -> int:
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _arg(name: str, t: torch.Tensor, dtype: torch.dtype, shape: tuple, dev: int) -> int:
+    """The address of a contiguous tensor of this dtype and shape on GPU `dev`."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise JabError(JAB_E_INVALID, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not "
                                       f"{t.dtype} {tuple(t.shape)}{'' if t.is_contiguous() else ' with strides'}")
-    if t.device.type != "cuda" or t.device.index != (torch.cuda.current_device() if device is None else device):
-        raise JabError(JAB_E_INVALID, f"{name} is on {t.device}, not on the current GPU")
+    if t.get_device() != dev:
+        raise JabError(JAB_E_INVALID, f"{name} is on {t.device}, not on GPU {dev}")
     return t.data_ptr()
 
 
@@ -412,16 +428,17 @@ def quant_rows(p: Problem, src: torch.Tensor, codes: Optional[torch.Tensor] = No
                scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows of d_model values (any leading dimensions) onto the symmetric 8-bit grid, a scale per row ->
     (codes int8 of src's shape, scale fp32 of its leading dimensions)."""
-    if src.dim() < 1 or src.shape[-1] != p.d_model:
-        raise JabError(JAB_E_INVALID, f"src must have rows of d_model = {p.d_model} values, not shape {tuple(src.shape)}")
-    sp = _arg("src", src, p.torch_dtype, src.shape)
+    d, shape = p.d_model, src.shape
+    if len(shape) < 1 or shape[-1] != d:
+        raise JabError(JAB_E_INVALID, f"src must have rows of d_model = {d} values, not shape {tuple(shape)}")
+    dev = _here(src)
+    sp = _arg("src", src, _CODE_DTYPE[p.dtype], shape, dev)
     if codes is None:
-        codes = torch.empty(src.shape, dtype=torch.int8, device=src.device)
+        codes = torch.empty_like(src, dtype=torch.int8)
     if scale is None:
-        scale = torch.empty(src.shape[:-1], dtype=torch.float32, device=src.device)
-    _check(lib().jab_quant_rows(ctypes.byref(p), src.numel() // p.d_model, sp,
-                                _arg("codes", codes, torch.int8, src.shape),
-                                _arg("scale", scale, torch.float32, src.shape[:-1]), _stream()))
+        scale = src.new_empty(shape[:-1], dtype=torch.float32)
+    _check(lib().jab_quant_rows(ctypes.byref(p), src.numel() // d, sp, _arg("codes", codes, torch.int8, shape, dev),
+                                _arg("scale", scale, torch.float32, shape[:-1], dev), _stream_of(dev)))
     return codes, scale
 
 
@@ -429,13 +446,13 @@ def project_int(p: Problem, xq: torch.Tensor, sx: torch.Tensor, wq: torch.Tensor
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The fused projection on 8-bit integers: codes xq [B][T][d_model], wq [R][d_model] and their rows'
     scales (quant_rows) -> y [B][T][R]."""
-    B, T, d = p.batch, p.seq_len, p.d_model
+    B, T, d, R, dt, dev = p.batch, p.seq_len, p.d_model, p.rows, _CODE_DTYPE[p.dtype], _here(xq)
     if out is None:
-        out = torch.empty((B, T, p.rows), dtype=p.torch_dtype, device=xq.device)
-    _check(lib().jab_project_int(ctypes.byref(p), _arg("xq", xq, torch.int8, (B, T, d)),
-                                 _arg("sx", sx, torch.float32, (B, T)), _arg("wq", wq, torch.int8, (p.rows, d)),
-                                 _arg("sw", sw, torch.float32, (p.rows,)),
-                                 _arg("out", out, p.torch_dtype, (B, T, p.rows)), _stream()))
+        out = xq.new_empty((B, T, R), dtype=dt)
+    _check(lib().jab_project_int(ctypes.byref(p), _arg("xq", xq, torch.int8, (B, T, d), dev),
+                                 _arg("sx", sx, torch.float32, (B, T), dev), _arg("wq", wq, torch.int8, (R, d), dev),
+                                 _arg("sw", sw, torch.float32, (R,), dev), _arg("out", out, dt, (B, T, R), dev),
+                                 _stream_of(dev)))
     return out
 
 
@@ -450,8 +467,9 @@ class Cache:
             raise JabError(JAB_E_INVALID, "zero-points go with the asymmetric scheme")
         self.tensors = (k, v, k_scale, v_scale, k_zero, v_zero)      # kept alive with the struct's addresses
         self.geometry = (h, p.head_dim, p.scheme)
-        self.device = k.device.index
-        dev = self.device
+        if not k.is_cuda:
+            raise JabError(JAB_E_INVALID, f"the cache is on {k.device}, not on a GPU")
+        self.device = dev = k.get_device()
         rows = (n, h, page_size)
         self.struct = _CacheStruct(
             bits, page_size, n, _arg("k", k, torch.uint8, rows + (dhb,), dev),
@@ -459,6 +477,7 @@ class Cache:
             _arg("k_scale", k_scale, torch.float32, rows, dev), _arg("v_scale", v_scale, torch.float32, rows, dev),
             None if k_zero is None else _arg("k_zero", k_zero, torch.uint8, rows, dev),
             None if v_zero is None else _arg("v_zero", v_zero, torch.uint8, rows, dev))
+        self.ref = ctypes.byref(self.struct)
 
     @classmethod
     def empty(cls, p: Problem, bits: int, page_size: int, n_pages: int, device="cuda") -> "Cache":
@@ -483,45 +502,50 @@ class CacheRows:
         if pages.dim() != 2:
             raise JabError(JAB_E_INVALID, "pages must be [n_seq][max_pages]")
         n = pages.shape[0]
-        self.device = pages.device.index
-        dev = self.device
+        if not pages.is_cuda:
+            raise JabError(JAB_E_INVALID, f"pages is on {pages.device}, not on a GPU")
+        self.device = dev = pages.get_device()
         self.tensors = (pages, past, start)
-        self.struct = _CacheRowsStruct(n, pages.shape[1], int(max_new), _arg("pages", pages, torch.int32, pages.shape, dev),
+        self.struct = _CacheRowsStruct(n, pages.shape[1], int(max_new),
+                                       _arg("pages", pages, torch.int32, pages.shape, dev),
                                        _arg("past", past, torch.int32, (n,), dev),
                                        _arg("start", start, torch.int32, (n + 1,), dev))
+        self.ref = ctypes.byref(self.struct)
 
 
-def _cache_call(p: Problem, cache: Cache, rows: CacheRows):
+def _cache_call(p: Problem, cache: Cache, rows: CacheRows) -> int:
+    """The GPU of a call on this cache and these rows."""
     if cache.geometry != (p.n_kv_heads, p.head_dim, p.scheme):
         raise JabError(JAB_E_INVALID, "the cache was laid out for other heads or another scheme")
-    if cache.device != torch.cuda.current_device() or rows.device != cache.device:
+    dev = torch.cuda.current_device()
+    if cache.device != dev or rows.device != dev:
         raise JabError(JAB_E_INVALID, "the cache and its rows must be on the current GPU")
-    return ctypes.byref(p), ctypes.byref(cache.struct), ctypes.byref(rows.struct)
+    return dev
 
 
 def cache_write(p: Problem, cache: Cache, rows: CacheRows, y: torch.Tensor) -> None:
     """The key (turned by the rotary embedding) and value columns of y [B][T][R] into the cache."""
-    a = _cache_call(p, cache, rows)
-    _check(lib().jab_cache_write(*a, _arg("y", y, p.torch_dtype, (p.batch, p.seq_len, p.rows)), _stream()))
+    dev = _cache_call(p, cache, rows)
+    _check(lib().jab_cache_write(ctypes.byref(p), cache.ref, rows.ref,
+                                 _arg("y", y, _CODE_DTYPE[p.dtype], (p.batch, p.seq_len, p.rows), dev), _stream_of(dev)))
 
 
 def cache_read(p: Problem, cache: Cache, rows: CacheRows, k: Optional[torch.Tensor] = None,
                v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """What cache_write stored for these rows -> (k, v) [B][T][n_kv_heads * head_dim] in the dtype."""
-    a = _cache_call(p, cache, rows)
-    shape = (p.batch, p.seq_len, p.n_kv_heads * p.head_dim)
-    dev = cache.tensors[0].device
+    dev, dt, shape = _cache_call(p, cache, rows), _CODE_DTYPE[p.dtype], (p.batch, p.seq_len, p.n_kv_heads * p.head_dim)
     if k is None:
-        k = torch.empty(shape, dtype=p.torch_dtype, device=dev)
+        k = cache.tensors[0].new_empty(shape, dtype=dt)
     if v is None:
-        v = torch.empty(shape, dtype=p.torch_dtype, device=dev)
-    _check(lib().jab_cache_read(*a, _arg("k", k, p.torch_dtype, shape), _arg("v", v, p.torch_dtype, shape), _stream()))
+        v = cache.tensors[0].new_empty(shape, dtype=dt)
+    _check(lib().jab_cache_read(ctypes.byref(p), cache.ref, rows.ref, _arg("k", k, dt, shape, dev),
+                                _arg("v", v, dt, shape, dev), _stream_of(dev)))
     return k, v
 
 
 def attn_cache_workspace(p: Problem, cache: Cache, rows: CacheRows) -> torch.Tensor:
     """The workspace attn_cache needs for this cache and these rows' sizes (possibly empty)."""
-    n = lib().jab_attn_cache_workspace(ctypes.byref(p), ctypes.byref(cache.struct), ctypes.byref(rows.struct))
+    n = lib().jab_attn_cache_workspace(ctypes.byref(p), cache.ref, rows.ref)
     if n == ctypes.c_size_t(-1).value:
         raise JabError(JAB_E_INVALID, lib().jab_last_error().decode())
     return torch.empty(n, dtype=torch.uint8, device=cache.tensors[0].device)
@@ -530,15 +554,15 @@ def attn_cache_workspace(p: Problem, cache: Cache, rows: CacheRows) -> torch.Ten
 def attn_cache(p: Problem, cache: Cache, rows: CacheRows, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of y's query columns over the cache -> [B][T][n_heads * head_dim] in the dtype."""
-    a = _cache_call(p, cache, rows)
-    shape = (p.batch, p.seq_len, p.n_heads * p.head_dim)
+    dev, dt, B, T = _cache_call(p, cache, rows), _CODE_DTYPE[p.dtype], p.batch, p.seq_len
+    shape = (B, T, p.n_heads * p.head_dim)
     if out is None:
-        out = torch.empty(shape, dtype=p.torch_dtype, device=y.device)
+        out = y.new_empty(shape)
     if ws is None:
         ws = attn_cache_workspace(p, cache, rows)
-    _check(lib().jab_attn_cache(*a, _arg("y", y, p.torch_dtype, (p.batch, p.seq_len, p.rows)),
-                                _arg("out", out, p.torch_dtype, shape),
-                                _arg("ws", ws, torch.uint8, ws.shape), ws.numel(), _stream()))
+    _check(lib().jab_attn_cache(ctypes.byref(p), cache.ref, rows.ref, _arg("y", y, dt, (B, T, p.rows), dev),
+                                _arg("out", out, dt, shape, dev), _arg("ws", ws, torch.uint8, ws.shape, dev), ws.numel(),
+                                _stream_of(dev)))
     return out
 
 
