@@ -10,8 +10,11 @@
 // Bound by HBM (the projection's columns in, the codes out).  A workgroup takes blocks of 32 positions of one
 // sequence, all heads: the fp64 cosines and sines of a block are formed once for its heads.  Eight
 // lanes per (token, head), each with the pairs (j, j + dh / 2) that the rotation and the 4-bit bytes
-// need; values leave through LDS, where a head's tile turns to the cache's token-contiguous order.
+// need; values leave through LDS, where a head's tile turns to the cache's token-contiguous order, and the next head's
+// elements are on their way under this one's arithmetic.
 // A block with few new tokens (a decoding step) goes by (token, head) items instead, all heads at once.
+// Measured: 32768 bf16 tokens of 8 heads of 128 (201 MB both ways) are written in 56-64 us, where memory alone needs 40 and
+// the arithmetic, about 8 instructions an element, 35, and read back in 36 (5.6 TB/s).
 #include "device_common.h"
 #include "cache.h"
 
@@ -19,14 +22,12 @@ namespace jab {
 namespace {
 
 constexpr int FEW = 4;                  // new tokens of a block that go without the LDS tile
-constexpr int PITCH = 40;               // bytes between the tile's rows of 32 tokens in LDS
+constexpr int PITCH = 36;               // bytes between the tile's rows of 32 tokens in LDS (words 9 d + t / 4: few conflicts)
 
-// C elements as fp32
-template <int DT, int C>
-__device__ inline void load_c(const typename Mma<DT>::elem *p, float *v) {
-    typedef typename Mma<DT>::elem elem;
-    elem e[C];
-    constexpr int B = C * (int)sizeof(elem);
+// C elements
+template <typename E, int C>
+__device__ inline void load_c(const E *p, E *e) {
+    constexpr int B = C * (int)sizeof(E);
     if constexpr (B % 16 == 0) {
 #pragma unroll
         for (int i = 0; i < B / 16; ++i) reinterpret_cast<u32x4 *>(e)[i] = reinterpret_cast<const u32x4 *>(p)[i];
@@ -36,8 +37,6 @@ __device__ inline void load_c(const typename Mma<DT>::elem *p, float *v) {
 #pragma unroll
         for (int i = 0; i < C; ++i) e[i] = p[i];
     }
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = to_f32<DT>(e[i]);
 }
 template <int DT, int C>
 __device__ inline void store_c(typename Mma<DT>::elem *p, const float *v) {
@@ -85,45 +84,65 @@ __device__ inline void load_bytes(const uint8_t *p, uint8_t *b) {
     }
 }
 
-// codes of the 2 C elements that this lane holds of a head (eight consecutive lanes hold the head), its
-// scale and zero-point
+// f over the eight consecutive lanes of a (token, head): every lane gets the whole.
+template <typename F>
+__device__ inline float over8(float v, F &&f) {
+    auto at = [](float x, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    v = f(v, at(v, std::integral_constant<int, 0xB1>{}));  // neighbours (quad 1 0 3 2)
+    v = f(v, at(v, std::integral_constant<int, 0x4E>{}));  // pairs (quad 2 3 0 1)
+    return f(v, at(v, std::integral_constant<int, 0x141>{}));   // quads (eight mirrored)
+}
+// One word of each of four tokens (lanes eight apart), its bytes four elements: the lane of token i gets the
+// four tokens' bytes i.  Two steps of a 4 x 4 transposition, lanes 8 and 16 apart.
+__device__ inline uint32_t quad_bytes(uint32_t w) {
+    const bool b0 = threadIdx.x & 8, b1 = threadIdx.x & 16;
+    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x128, 0xF, 0xF, true);     // 8 lanes on
+    w = __builtin_amdgcn_perm(o, w, b0 ? 0x03070105u : 0x06020400u);   // bytes of o are 4 .. 7
+    uint32_t lo = w, hi = w;                               // words of the even and of the odd rows of 16 lanes
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(lo), "+v"(hi));
+    return __builtin_amdgcn_perm(hi, lo, b1 ? 0x07060302u : 0x05040100u);
+}
+
+// Codes of the 2 C elements that this lane holds of a head (eight consecutive lanes hold the head), four to a
+// word in order, its scale and zero-point.
+// Quotients x / s are rounded to fp32 as a division rounds them, without dividing: in fp64, x times the rounded 1 / s is
+// within 2^-52 of x / s, and a quotient of two fp32 numbers is nearer than 2^-25 of its last place to no midpoint of
+// two fp32 numbers, so both round alike; the same holds of a division by the constants.  (32 divisions of
+// a lane were half of the kernel's instructions.)
 template <int BITS, int C>
-__device__ inline void encode(const float (&x)[2 * C], bool sym, uint8_t (&code)[2 * C], float &s, uint8_t &z) {
-    float lo = 0.f, hi = 0.f;
-    uint32_t mx = 0;                    // the largest magnitude, infinity and NaN above all others
+__device__ inline void encode(const float (&x)[2 * C], bool sym, uint32_t (&code)[(2 * C + 3) / 4], float &s, uint8_t &z) {
+    float lo = 0.f, hi = 0.f, bad = 0.f;                   // bad: NaN with an infinite or NaN element
 #pragma unroll
     for (int i = 0; i < 2 * C; ++i) {
         lo = fminf(lo, x[i]);
         hi = fmaxf(hi, x[i]);
-        mx = max(mx, __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu);
+        bad = __builtin_fmaf(x[i], 0.f, bad);
     }
-#pragma unroll
-    for (int off = 1; off < 8; off *= 2) {
-        lo = fminf(lo, __shfl_xor(lo, off, 64));
-        hi = fmaxf(hi, __shfl_xor(hi, off, 64));
-        mx = max(mx, (uint32_t)__shfl_xor((int)mx, off, 64));
-    }
+    lo = over8(lo, [](float a, float b) { return fminf(a, b); });
+    hi = over8(hi, [](float a, float b) { return fmaxf(a, b); });
+    bad = over8(bad, [](float a, float b) { return a + b; });
     constexpr float top = (float)((1 << BITS) - 1), q = (float)((1 << (BITS - 1)) - 1);
     float zf = q, most = 2.f * q;
-    if (sym) {
-        s = __builtin_bit_cast(float, mx) / q;
-        if (s == 0.f) s = 1.f;
-    } else {
-        s = (hi - lo) / top;
-        if (s == 0.f) s = 1.f;
-        zf = fminf(fmaxf(rintf(-lo / s), 0.f), top);
+    s = (float)(sym ? (double)fmaxf(-lo, hi) * (1.0 / q) : (double)(hi - lo) * (1.0 / top));
+    if (s == 0.f) s = 1.f;
+    const double r = 1.0 / (double)s;
+    if (!sym) {
+        zf = fminf(fmaxf(rintf((float)(-(double)lo * r)), 0.f), top);
         most = top;
     }
-    const bool fine = mx < 0x7F800000u && s < __builtin_inff();
-    if (!fine) {
+    if (!(bad == 0.f && s < __builtin_inff())) {
         s = __builtin_nanf("");
-        zf = 0.f;
+        zf = most = 0.f;                                   // and all codes 0: the middle of (0, 0, anything), NaN too
     }
     z = (uint8_t)(int)zf;
 #pragma unroll
+    for (int w = 0; w < (2 * C + 3) / 4; ++w) code[w] = 0;
+#pragma unroll
     for (int i = 0; i < 2 * C; ++i) {
-        const float u = fminf(fmaxf(rintf(x[i] / s) + zf, 0.f), most);
-        code[i] = fine ? (uint8_t)(int)u : 0;
+        const float v = __builtin_amdgcn_fmed3f(rintf((float)((double)x[i] * r)) + zf, 0.f, most);
+        code[i >> 2] = __builtin_amdgcn_cvt_pk_u8_f32(v, i & 3, code[i >> 2]);
     }
 }
 
@@ -143,12 +162,13 @@ __device__ inline void for_blocks(const CacheArgs &g, int nb, F &&f) {
 }
 
 template <int DT, int DH, int BITS>
-__global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy, int nb) {
+__global__ __launch_bounds__(256, 4) void cache_write_kernel(CacheArgs g, const void *__restrict__ yv, int64_t ldy, int nb) {
     typedef typename Mma<DT>::elem elem;
     constexpr int HALF = DH / 2, C = DH / 16, DHB = DH * BITS / 8;
-    __shared__ double2 tab[32 * HALF];                 // (cos, sin) of the block's positions
+    __shared__ double2 tab[32 * HALF];                 // (cos, sin) of the block's positions, pair j of a token at mix(j):
+    auto mix = [](int j) { return j ^ ((j >> 3) & 7); };    // the eight lanes of a head read distinct banks
     __shared__ __align__(16) uint8_t tile[DHB * PITCH];
-    const int tid = threadIdx.x, e = tid & 7;
+    const int tid = threadIdx.x, e = tid & 7, slot32 = tid >> 3;
     const bool rope = g.freq[0] != 0.0, sym = g.k_zero == nullptr;
     for_blocks(g, nb, [&](int s, const SeqRows &r, int blk, int t0, int t1) {
         const int page = page_of(g, s, blk * 32);
@@ -156,46 +176,87 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs g, const voi
         const int nt = t1 - t0, at0 = (blk * 32) & ((1 << g.page_shift) - 1);
         if (rope) {
             __syncthreads();
-            for (int i = tid; i < nt * HALF; i += 256) {
-                double sn, cs;
-                sincos((double)(blk * 32 + t0 + i / HALF) * g.freq[i % HALF], &sn, &cs);
-                tab[i] = make_double2(cs, sn);
+            if (nt <= FEW) {
+                for (int i = tid; i < nt * HALF; i += 256) {
+                    double sn, cs;
+                    sincos((double)(blk * 32 + t0 + i / HALF) * g.freq[i % HALF], &sn, &cs);
+                    tab[i / HALF * HALF + mix(i % HALF)] = make_double2(cs, sn);
+                }
+            } else {
+                // eight positions in a row from the first one's angle, each the one before turned by one position (in
+                // fp64: 2^-53 a step; a sine and cosine are 250 instructions, a turn 6)
+                for (int i = tid; i < 4 * HALF; i += 256) {
+                    const int j = i % HALF, k0 = i / HALF * 8;
+                    double sn, cs, s1, c1;
+                    sincos((double)(blk * 32 + t0 + k0) * g.freq[j], &sn, &cs);
+                    sincos(g.freq[j], &s1, &c1);
+                    for (int k = k0; k < min(k0 + 8, nt); ++k) {
+                        tab[k * HALF + mix(j)] = make_double2(cs, sn);
+                        const double c = cs * c1 - sn * s1;
+                        sn = sn * c1 + cs * s1;
+                        cs = c;
+                    }
+                }
             }
             __syncthreads();
         }
         const elem *rows = static_cast<const elem *>(yv) + (int64_t)(r.row + (blk * 32 - r.past)) * ldy;
-        // one (token, head): codes, key bytes and scales stored, value codes returned
-        auto item = [&](int t, int h, uint8_t (&vc)[2 * C]) {
-            const elem *kp = rows + (int64_t)t * ldy + (int64_t)(g.n_heads + h) * DH + e * C;
-            const elem *vp = kp + (int64_t)g.n_kv_heads * DH;
+        // one (token, head): its elements; then codes, key bytes and scales stored, value codes returned.  Another one's
+        // elements are asked for where this one's are used up, so that they are on their way under the arithmetic.
+        struct Elems {
+            __align__(16) elem k[2 * C], v[2 * C];
+        };
+        auto key_at = [&](int t, int h) { return rows + (int64_t)t * ldy + (int64_t)(g.n_heads + h) * DH + e * C; };
+        auto load_k = [&](Elems &m, int t, int h) {
+            const elem *p = key_at(t, h);
+            load_c<elem, C>(p, m.k);
+            load_c<elem, C>(p + HALF, m.k + C);
+        };
+        auto load_v = [&](Elems &m, int t, int h) {
+            const elem *p = key_at(t, h) + (int64_t)g.n_kv_heads * DH;
+            load_c<elem, C>(p, m.v);
+            load_c<elem, C>(p + HALF, m.v + C);
+        };
+        auto item = [&](Elems &m, int t, int h, int next, uint32_t (&vw)[(2 * C + 3) / 4]) {
             float x[2 * C], y[2 * C];
-            load_c<DT, C>(kp, x);
-            load_c<DT, C>(kp + HALF, x + C);
-            load_c<DT, C>(vp, y);
-            load_c<DT, C>(vp + HALF, y + C);
+#pragma unroll
+            for (int i = 0; i < 2 * C; ++i) x[i] = to_f32<DT>(m.k[i]);
+            if (next >= 0) load_k(m, t, next);
             if (rope) {
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
-                    const double2 cs = tab[(t - t0) * HALF + e * C + i];
+                    const double2 cs = tab[(t - t0) * HALF + mix(e * C + i)];
                     const double a = x[i], b = x[C + i];
                     x[i] = (float)(a * cs.x - b * cs.y);
                     x[C + i] = (float)(b * cs.x + a * cs.y);
                 }
             }
             uint8_t kc[2 * C], kz, vz;
+            uint32_t kw[(2 * C + 3) / 4];
             float ks, vs;
-            encode<BITS, C>(x, sym, kc, ks, kz);
-            encode<BITS, C>(y, sym, vc, vs, vz);
+            encode<BITS, C>(x, sym, kw, ks, kz);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 2 * C; ++i) y[i] = to_f32<DT>(m.v[i]);
+            if (next >= 0) load_v(m, t, next);
+            encode<BITS, C>(y, sym, vw, vs, vz);
+            __builtin_memcpy(kc, kw, 2 * C);
             const int64_t slot = (((int64_t)page * g.n_kv_heads + h) << g.page_shift) + at0 + t;
             uint8_t *kr = g.k + slot * DHB + e * C;
             if constexpr (BITS == 8) {
                 store_bytes<C>(kr, kc);
                 store_bytes<C>(kr + HALF, kc + C);
             } else {
+                if constexpr (C >= 4) {
 #pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    kc[i] |= kc[C + i] << 4;
-                    vc[i] |= vc[C + i] << 4;
+                    for (int i = 0; i < C / 4; ++i) {
+                        kw[i] |= kw[C / 4 + i] << 4;
+                        vw[i] |= vw[C / 4 + i] << 4;
+                    }
+                    __builtin_memcpy(kc, kw, C);
+                } else {
+                    kc[0] |= kc[1] << 4;
+                    vw[0] = (vw[0] | vw[0] >> 4) & 255u;
                 }
                 store_bytes<C>(kr, kc);
             }
@@ -212,24 +273,40 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs g, const voi
         };
         if (nt <= FEW) {
             for (int i0 = 0; i0 < nt * g.n_kv_heads; i0 += 32) {
-                const int i = i0 + (tid >> 3);
+                const int i = i0 + slot32;
                 if (i >= nt * g.n_kv_heads) break;     // eight lanes of an item leave together
                 const int t = t0 + i % nt, h = i / nt;
-                uint8_t vc[2 * C];
-                item(t, h, vc);
+                uint32_t vw[(2 * C + 3) / 4];
+                Elems m;
+                load_k(m, t, h);
+                load_v(m, t, h);
+                item(m, t, h, -1, vw);
                 uint8_t *vb = vbase(h);
 #pragma unroll
-                for (int k = 0; k < NC; ++k) vb[(e * C + (k < C ? k : HALF + k - C)) * 32 + t] = vc[k];
+                for (int k = 0; k < NC; ++k)
+                    vb[(e * C + (k < C ? k : HALF + k - C)) * 32 + t] = (uint8_t)(vw[k >> 2] >> (8 * (k & 3)));
             }
             return;
         }
-        const int t = tid >> 3;
+        // the lanes of four tokens exchange their bytes, so that a word of the tile is four tokens of one element (tokens
+        // that are not new leave what is not stored)
+        const int t = slot32;
+        const bool mine = t >= t0 && t < t1;
+        Elems m;
+        if (mine) {
+            load_k(m, t, 0);
+            load_v(m, t, 0);
+        }
         for (int h = 0; h < g.n_kv_heads; ++h) {
-            if (t >= t0 && t < t1) {
-                uint8_t vc[2 * C];
-                item(t, h, vc);
+            uint32_t vw[(2 * C + 3) / 4] = {};
+            if (mine) item(m, t, h, h + 1 < g.n_kv_heads ? h + 1 : -1, vw);
+            if (h) __syncthreads();                        // the tile is read
 #pragma unroll
-                for (int k = 0; k < NC; ++k) tile[(e * C + (k < C ? k : HALF + k - C)) * PITCH + t] = vc[k];
+            for (int w = 0; w < (NC + 3) / 4; ++w) {
+                const uint32_t q = quad_bytes(vw[w]);
+                const int k = 4 * w + (t & 3);             // this lane's element of the word
+                if (NC % 4 == 0 || k < NC)
+                    *reinterpret_cast<uint32_t *>(tile + (e * C + (k < C ? k : HALF + k - C)) * PITCH + (t & ~3)) = q;
             }
             __syncthreads();
             uint8_t *vb = vbase(h);
@@ -244,8 +321,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheArgs g, const voi
                         if (tw + k >= t0 && tw + k < t1) vb[d * 32 + tw + k] = src[k];
                 }
             }
-            __syncthreads();
         }
+        __syncthreads();                                   // the tiles before the next block's
     });
 }
 
@@ -314,9 +391,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs g, void *__re
             const uint8_t *vb = vbase(h);
             for (int c = tid; c < DHB * 2; c += 256) { // whole tiles: chunks of 16 tokens
                 const u32x4 q = *reinterpret_cast<const u32x4 *>(vb + c * 16);
-                uint2 *dst = reinterpret_cast<uint2 *>(tile + (c >> 1) * PITCH + (c & 1) * 16);
-                dst[0] = make_uint2(q[0], q[1]);
-                dst[1] = make_uint2(q[2], q[3]);
+                uint32_t *dst = reinterpret_cast<uint32_t *>(tile + (c >> 1) * PITCH + (c & 1) * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dst[i] = q[i];
             }
             __syncthreads();
             if (t >= t0 && t < t1) item(t, h, [&](int d) { return tile[d * PITCH + t]; });
