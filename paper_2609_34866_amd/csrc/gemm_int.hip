@@ -83,19 +83,21 @@ __global__ __launch_bounds__(NT) void quant_rows_kernel(const void *__restrict__
         for (int i = 0; i < NT / 64; ++i) mx = max(mx, part[i]);
     }
     const bool fine = mx < 0x7F800000u;
-    float s = __builtin_bit_cast(float, mx) / 127.f;
+    // quotients as a division rounds them, without dividing: x times the fp64 reciprocal is within 2^-52 of x / s, which
+    // is nearer than 2^-25 of its last place to no midpoint of two fp32 numbers, so both round alike
+    float s = (float)((double)__builtin_bit_cast(float, mx) * (1.0 / 127));
     if (s == 0.f) s = 1.f;
-    if (!fine) s = __builtin_nanf("");
-    if (threadIdx.x == 0) scale[row] = s;
+    const double r = 1.0 / (double)s;
+    const float most = fine ? 127.f : 0.f;                 // codes 0 where the scale is NaN
+    if (threadIdx.x == 0) scale[row] = fine ? s : __builtin_nanf("");
     auto put = [&](int c, const float *x) {
         uint32_t o[2] = {0, 0};
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float u = fminf(fmaxf(rintf(x[k] / s), -127.f), 127.f);
-            const int q = fine ? (int)u : 0;
-            o[k >> 2] |= (uint32_t)(q & 255) << (8 * (k & 3));
+            const float u = __builtin_amdgcn_fmed3f(rintf((float)((double)x[k] * r)), -most, most);
+            o[k >> 2] = __builtin_amdgcn_cvt_pk_u8_f32(u + 128.f, k & 3, o[k >> 2]);
         }
-        *reinterpret_cast<uint2 *>(codes + e0 + (int64_t)c * 8) = make_uint2(o[0], o[1]);
+        *reinterpret_cast<uint2 *>(codes + e0 + (int64_t)c * 8) = make_uint2(o[0] ^ 0x80808080u, o[1] ^ 0x80808080u);
     };
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -427,64 +429,76 @@ __global__ __launch_bounds__(256, 1) void int_w4p_kernel(IntArgs g) {
     wait_vmcnt<0>();
 }
 
-// Few tokens: a workgroup takes 16 weight rows, its eight waves each an eighth of K (in steps of 64 codes:
-// v_mfma_i32_16x16x64_i8, lane (row l % 16, g = l / 16) holding codes 16 g .. 16 g + 15 of the step).  Weights
-// and tokens go from memory to registers, UNR steps at once; the sums of the waves meet in LDS.  Bound by the
-// weights' bytes: few rows per workgroup, so that every CU has some.
+// Few tokens: a workgroup takes 16 RT weight rows and all tokens (16 MT), its eight waves each an eighth of K (in steps of
+// 64 codes: v_mfma_i32_16x16x64_i8, lane (row l % 16, g = l / 16) holding codes 16 g .. 16 g + 15 of the step).  Weights
+// and tokens go from memory to registers, UNR steps at once; the sums of the waves meet in LDS.  Bound by the bytes
+// that a CU takes in: every workgroup reads all tokens' codes over.  32 tokens, 6144 rows, K 4096 (25 MB of weights):
+// 12.5 us with RT 1, 9.9 with the 2 that the rule takes; a device copy of as many bytes takes 7.7.  More steps at once, nontemporal
+// loads or another order of the steps changed nothing.
 constexpr int SK_WAVES = 8;
-template <int DT, int MT>
+template <int DT, int RT, int MT>
 __global__ __launch_bounds__(64 * SK_WAVES) void int_skinny_kernel(IntArgs g) {
     typedef typename Mma<DT>::elem elem;
-    constexpr int UNR = 4;
-    __shared__ i32x4 red[SK_WAVES][MT][64];
+    static_assert(RT * MT <= SK_WAVES, "one wave per tile at the end");
+    constexpr int UNR = RT * MT == 8 ? 2 : 4;
+    __shared__ i32x4 red[SK_WAVES][RT * MT][64];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int l16 = lane & 15, grp = lane >> 4;
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * 16 * RT;
     const int steps = (g.K + 63) / 64;
     const int s0 = (int)((int64_t)steps * wave / SK_WAVES), s1 = (int)((int64_t)steps * (wave + 1) / SK_WAVES);
-    const int8_t *wp = g.B + (int64_t)(n0 + l16) * g.K + grp * 16;
-    const int8_t *xp[MT];
+    const int8_t *wp[RT], *xp[MT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) wp[r] = g.B + (int64_t)min(n0 + 16 * r + l16, g.N - 1) * g.K + grp * 16;
 #pragma unroll
     for (int t = 0; t < MT; ++t) xp[t] = g.A + (int64_t)min(16 * t + l16, g.M - 1) * g.K + grp * 16;
-    i32x4 acc[MT];
+    i32x4 acc[RT][MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[r][t] = i32x4{0, 0, 0, 0};
     for (int s = s0; s < s1; s += UNR) {
-        i32x4 w[UNR], x[UNR][MT];
+        i32x4 w[UNR][RT], x[UNR][MT];
 #pragma unroll
         for (int u = 0; u < UNR; ++u) {
             const int k = 64 * (s + u);
             // past the wave's share, or the last 32 of a K that is no multiple of 64: zeros for the weights
             // (any codes for the tokens)
             const bool in = s + u < s1 && k + 16 * grp < g.K;
-            const int at = in ? k : 0;
-            w[u] = *reinterpret_cast<const i32x4 *>(wp + (in ? at : -16 * grp));
-            if (!in) w[u] = i32x4{0, 0, 0, 0};
+            const int at = in ? k : -16 * grp;
 #pragma unroll
-            for (int t = 0; t < MT; ++t) x[u][t] = *reinterpret_cast<const i32x4 *>(xp[t] + (in ? at : -16 * grp));
+            for (int r = 0; r < RT; ++r) {
+                w[u][r] = *reinterpret_cast<const i32x4 *>(wp[r] + at);
+                if (!in) w[u][r] = i32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) x[u][t] = *reinterpret_cast<const i32x4 *>(xp[t] + at);
         }
 #pragma unroll
         for (int u = 0; u < UNR; ++u)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], x[u][t], acc[t], 0, 0, 0);
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][r], x[u][t], acc[r][t], 0, 0, 0);
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t) red[wave][t][lane] = acc[t];
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) red[wave][r * MT + t][lane] = acc[r][t];
     __syncthreads();
-    // acc[t][i]: token 16 t + l16, weight row n0 + 4 grp + i
-    if (wave < MT) {
-        const int t = wave;
-        i32x4 s = red[0][t][lane];
+    // acc[r][t][i]: token 16 t + l16, weight row n0 + 16 r + 4 grp + i
+    if (wave < RT * MT) {
+        i32x4 s = red[0][wave][lane];
 #pragma unroll
         for (int w = 1; w < SK_WAVES; ++w) {
-            const i32x4 v = red[w][t][lane];
+            const i32x4 v = red[w][wave][lane];
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[e] += v[e];
         }
-        const int m = 16 * t + l16;
-        if (m < g.M) {
-            const int n = n0 + 4 * grp;
+        const int m = 16 * (wave % MT) + l16, n = n0 + 16 * (wave / MT) + 4 * grp;
+        if (m < g.M && n < g.N) {
             const f32x4 o = scaled4(s[0], s[1], s[2], s[3], g.sa[m], *reinterpret_cast<const f32x4 *>(g.sb + n));
             elem *c = static_cast<elem *>(g.C) + (int64_t)m * g.N + n;
             if constexpr (DT == F32) *reinterpret_cast<f32x4 *>(c) = o;
@@ -509,15 +523,26 @@ hipError_t run_small(IntArgs a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// The weight rows of a workgroup: what a CU takes in is, per workgroup that it gets, RT + MT tiles of 16 rows; the RT
+// with the least of it.
+template <int DT, int MT>
+hipError_t run_skinny(IntArgs a, hipStream_t st) {
+    const int tiles = (a.N + 15) / 16;
+    auto groups = [&](int rt) { return (tiles + rt - 1) / rt; };
+    auto cost = [&](int rt) { return (int64_t)((groups(rt) + CUS - 1) / CUS) * (rt + MT); };
+    int rt = cost(2) < cost(1) ? 2 : 1;
+    if (MT <= 2 && cost(4) < cost(rt)) rt = 4;
+    if (rt == 1) int_skinny_kernel<DT, 1, MT><<<groups(1), 64 * SK_WAVES, 0, st>>>(a);
+    else if (rt == 2) int_skinny_kernel<DT, 2, MT><<<groups(2), 64 * SK_WAVES, 0, st>>>(a);
+    else if constexpr (MT <= 2) int_skinny_kernel<DT, 4, MT><<<groups(4), 64 * SK_WAVES, 0, st>>>(a);
+    return hipGetLastError();
+}
+
 template <int DT>
 hipError_t run_int(IntArgs a, hipStream_t st) {
-    if (a.M <= 64) {
-        const dim3 grid(a.N / 16);
-        if (a.M <= 16) int_skinny_kernel<DT, 1><<<grid, 64 * SK_WAVES, 0, st>>>(a);
-        else if (a.M <= 32) int_skinny_kernel<DT, 2><<<grid, 64 * SK_WAVES, 0, st>>>(a);
-        else int_skinny_kernel<DT, 4><<<grid, 64 * SK_WAVES, 0, st>>>(a);
-        return hipGetLastError();
-    }
+    if (a.M <= 16) return run_skinny<DT, 1>(a, st);
+    if (a.M <= 32) return run_skinny<DT, 2>(a, st);
+    if (a.M <= 64) return run_skinny<DT, 4>(a, st);
     const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256, t = tm * tn;
     // the 256-tiles where they fill their rounds of one workgroup per CU to at least 70 %
     if (a.M >= 256 && a.N >= 256 && a.K % 128 == 0 && a.K >= 1024 && 10 * t >= 7 * ((t + CUS - 1) / CUS) * CUS) {
@@ -543,7 +568,10 @@ hipError_t run_quant_rows(int64_t rows, int cols, const void *src, int8_t *codes
     for (int64_t r = 0; r < rows; r += MOST_GROUPS) {
         const dim3 grid((unsigned)std::min(rows - r, MOST_GROUPS));
         const void *x = static_cast<const typename Mma<DT>::elem *>(src) + r * cols;
+        // eight elements a thread; 8000 rows of 768 fp16: 6.0 us with 128 threads, 7.4 with 256, 6.2 with 64 twice; 32 rows
+        // of 4096 bf16 (twice with 256): 3.4 us, 4.4 with 128 four times, 3.3 with 512; 16384: 71, 78 and 83 us (5.7 TB/s)
         if (cols <= 512) quant_rows_kernel<DT, 64, 1><<<grid, 64, 0, st>>>(x, cols, codes + r * cols, scale + r);
+        else if (cols <= 1024) quant_rows_kernel<DT, 128, 1><<<grid, 128, 0, st>>>(x, cols, codes + r * cols, scale + r);
         else quant_rows_kernel<DT, 256, 2><<<grid, 256, 0, st>>>(x, cols, codes + r * cols, scale + r);
     }
     return hipGetLastError();
