@@ -99,7 +99,16 @@ struct Lay {
 
 // from a wave-uniform base and a lane's byte offset
 template <typename T>
-__device__ inline T ldu(const uint8_t *base, uint32_t off) { return *reinterpret_cast<const T *>(base + off); }
+__device__ inline T ldu(const uint8_t *base, uint32_t off) {
+    asm("" : "+v"(off));                                   // widened at the load: else kept widened, twice the registers
+    return *reinterpret_cast<const T *>(base + off);
+}
+// the same of bytes that one workgroup reads, once: few rows 64 x 8 heads 103 us instead of 107, one of 130000 tokens 37
+// instead of 38.5 (many rows, whose blocks several workgroups read, 664 instead of 600)
+template <typename T>
+__device__ inline T ldu_once(const uint8_t *base, uint32_t off) {
+    return __builtin_nontemporal_load(reinterpret_cast<const T *>(base + off));
+}
 
 // where block blk of a sequence lies: its first slot, or -1
 __device__ inline int64_t block_slot(const CacheArgs &g, int s, int h, int blk) {
@@ -621,24 +630,24 @@ __global__ __launch_bounds__(256, OCC) void attn_few_kernel(CacheArgs g, const v
 #pragma unroll
                 for (int u = 0; u < L::KU; u += 2) {
                     if constexpr (L::KU >= 2) {            // two units are 16 bytes
-                        const u32x4 q = ldu<u32x4>(kb, koff + 4 * t * L::DHB + 64 * (u >> 1));
+                        const u32x4 q = ldu_once<u32x4>(kb, koff + 4 * t * L::DHB + 64 * (u >> 1));
                         k[t][u] = u32x2{q[0], q[1]};
                         k[t][u + 1] = u32x2{q[2], q[3]};
                     } else {
-                        k[t][0] = ldu<u32x2>(kb, koff + 4 * t * L::DHB);
+                        k[t][0] = ldu_once<u32x2>(kb, koff + 4 * t * L::DHB);
                     }
                 }
-                if (asym) kz[t] = ldu<uint8_t>(g.k_zero + slot, zoff + 4 * t);
-                ks[t] = ldu<f32x4>(sb, 32 * grp + 16 * t);
+                if (asym) kz[t] = ldu_once<uint8_t>(g.k_zero + slot, zoff + 4 * t);
+                ks[t] = ldu_once<f32x4>(sb, 32 * grp + 16 * t);
             }
         };
         auto load_v = [&](int64_t slot) {
             const uint8_t *vb = g.v + slot * L::DHB, *sb = reinterpret_cast<const uint8_t *>(g.v_scale + slot);
 #pragma unroll
-            for (int u = 0; u < L::VU; ++u) v[u] = ldu<u32x2>(vb, voff + 512 * u);
+            for (int u = 0; u < L::VU; ++u) v[u] = ldu_once<u32x2>(vb, voff + 512 * u);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) vs[t] = ldu<f32x4>(sb, 32 * grp + 16 * t);
-            if (asym) vz = ldu<u32x2>(g.v_zero + slot, 8 * grp);
+            for (int t = 0; t < 2; ++t) vs[t] = ldu_once<f32x4>(sb, 32 * grp + 16 * t);
+            if (asym) vz = ldu_once<u32x2>(g.v_zero + slot, 8 * grp);
         };
         // blocks wave, wave + 4, ... of the piece, the first one's bytes on their way before the queries are made; a
         // block without a page, and past the end, loads page 0 and is not used
@@ -897,7 +906,7 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
         __syncthreads();
 
         // block b's scores (scaled and masked) and value scales, as the loop's body for b wants them
-        constexpr int NQ = 2 * L::KS;
+        constexpr int NQ = 2 * L::KS, PF = 2;              // operands read ahead (3 or 4: no faster)
         f32x4 st[RT][2];
         float vs[8];
         auto operand = [&](const unsigned char *blk, int i) { return *reinterpret_cast<const f16x8 *>(blk + i * 1024 + lane * 16); };
@@ -931,22 +940,22 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
         for (int b = b0; b < end; ++b) {
             const unsigned char *cur = smem + slot, *nxt = smem + next(slot);
             unsigned char *fill = smem + next(next(slot));
-            const int ahead = page_at(b + 5);
             f16x8 op[NQ > L::NT ? NQ : L::NT];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) op[i] = operand(nxt, i);
+            for (int i = 0; i < PF; ++i) op[i] = operand(nxt, i);
             w.move(st, vs);
             const float up = w.up();
 #pragma unroll
             for (int i = 0; i < 8; ++i) vs[i] *= up;
             __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);                 // before the other workgroup's waves, which wait for theirs
             // the next block's scores (past the end: of what the ring holds, not used) beside this block's weights
             f32x4 sn[RT][2];
             f16x8 pw[RT][W::NP], vo[L::NT];
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
-                if (i + 2 < NQ) op[i + 2] = operand(nxt, i + 2);
-                else if (i + 2 - NQ < L::NT) vo[i + 2 - NQ] = operand(cur, S::KOPS + i + 2 - NQ);
+                if (i + PF < NQ) op[i + PF] = operand(nxt, i + PF);
+                else if (i + PF - NQ < L::NT) vo[i + PF - NQ] = operand(cur, S::KOPS + i + PF - NQ);
                 product(sn, i, op[i]);
 #pragma unroll
                 for (int j = i * 4 * RT / NQ; j < (i + 1) * 4 * RT / NQ; ++j) w.weight2(j, st, vs, pw);
@@ -957,7 +966,7 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
             turn_zero(raw);
 #pragma unroll
             for (int t = 0; t < L::NT; ++t) {
-                if (t + 2 < L::NT) vo[t + 2] = operand(cur, S::KOPS + t + 2);
+                if (t + PF < L::NT) vo[t + PF] = operand(cur, S::KOPS + t + PF);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -969,6 +978,8 @@ __global__ __launch_bounds__(256, 2) void attn_many_kernel(CacheArgs g, const vo
                     for (int i = 0; i < 4; ++i) sc4[i] = scales(nxt, i);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            __builtin_amdgcn_s_setprio(0);
+            const int ahead = page_at(b + 5);              // (here: no wait for LDS before the barrier waits for it too)
             turn_scales(raw, fill);
             load(raw, b + 3, pg[3]);
             const f32x4 ksn[2] = {sc4[0], sc4[1]};
