@@ -154,7 +154,8 @@ __device__ inline void for_blocks(const CacheArgs &g, int nb, F &&f) {
         const int s = (int)(it / nb);
         const SeqRows r = seq_rows(g, s);
         const int end = (int)min((int64_t)r.past + r.n, (int64_t)g.cap);
-        for (int blk = (r.past >> 5) + (int)(it % nb); blk * 32 < end; blk += nb) {
+        for (int64_t at = (r.past >> 5) + it % nb; at * 32 < end; at += nb) {        // (a step may pass 32 bits of positions)
+            const int blk = (int)at;
             const int t0 = max(r.past - blk * 32, 0), t1 = min(end - blk * 32, 32);
             if (t0 < t1) f(s, r, blk, t0, t1);
         }
