@@ -429,8 +429,12 @@ __device__ inline void store4(typename Mma<DT>::elem *p, f32x4 v) {
 // the tile begins here), which attn_join_kernel joins.
 constexpr int SNAP = 8, SHARE = 8;      // least blocks of a piece, of a share
 constexpr int SCAN_SEQS = 512;          // sequences up to which each workgroup scans them; past it one workgroup per
-                                        // (sequence, head), of which there are then enough
-constexpr int WHOLE = 48;               // blocks below which a (sequence, head) goes to one workgroup
+                                        // (sequence, head), of which there are then enough (1024 x 8 of 1600 tokens: 581 us,
+                                        // 634 with shares; 512: 285 and 313, but uneven lengths want them)
+// Blocks, over all tiles of a (sequence, head), below which it goes to one workgroup: shares cost their scan and the
+// join's launch.  One new token, whole / shares: 800 tokens 12.4 / 13.9 us, 1500 17.2 / 16.1, 6000 50 / 15; 16 sequences
+// 14.7 / 20.5, 25.2 / 25.4, 84 / 48.  128 rows on 432 tokens 25.0 / 28.0, on 832 36.6 / 25.7; 2048 rows on 512 268 / 49.
+constexpr int WHOLE_FEW = 48, WHOLE_MANY = 20;
 
 template <int ROWS>
 __device__ inline int tile_blocks(const CacheArgs &g, const SeqRows &r, int G, int tile) {
@@ -1124,18 +1128,21 @@ Plan plan_of(int dtype, const CacheArgs &g) {
     Plan p;
     const int G = g.n_heads / g.n_kv_heads;
     const int64_t rows = (int64_t)std::max(g.max_new, 1) * G, blocks = ((int64_t)g.cap + 31) / 32;
+    // (33 .. 64 rows as two few tiles: fp16 50 instead of 59 us at 8 x 4000 tokens, but bf16 213 instead of 192 at 64 x 4000
+    // and 31 instead of 23 at 8 x 400)
     p.few = rows <= 32;
     p.rt = rows <= 16 ? 1 : 2;
     p.rows = p.few ? 16 * p.rt : 128;
     const int64_t pairs = (int64_t)g.n_seq * g.n_kv_heads, tiles = (rows + p.rows - 1) / p.rows;
-    // Equal shares cost the scan and the join's launch; not where a (sequence, head) is short, nor where there are
-    // too many sequences to scan (and so enough workgroups).  A head's blocks of all sequences fit 32 bits, whatever
-    // the device finds (the tiles of all rows, and a ragged one per sequence).
-    p.scan = blocks >= WHOLE && g.n_seq <= SCAN_SEQS && ((int64_t)g.M * G / p.rows + g.n_seq) * blocks < INT32_MAX;
+    // Equal shares, but not where a (sequence, head) is short, nor where there are too many sequences to scan.  A head's
+    // blocks of all sequences fit 32 bits (the tiles of all rows, and a ragged one per sequence).
+    p.scan = tiles * blocks >= (p.few ? WHOLE_FEW : WHOLE_MANY) && g.n_seq <= SCAN_SEQS &&
+             ((int64_t)g.M * G / p.rows + g.n_seq) * blocks < INT32_MAX;
     p.many_pieces = false;
     p.groups = (int)pairs;
     if (!p.scan) return p;
-    // one round of the workgroups that the CUs hold at once; fewer where the shares would be short
+    // one round of the workgroups that the CUs hold at once; fewer where the shares would be short (two rounds: one
+    // sequence of 130000 tokens 53 us instead of 43)
     const int64_t slots = (int64_t)CUS * (p.few && p.rt == 1 && dtype == BF16 ? 3 : 2);
     p.groups = (int)std::min(slots, std::max<int64_t>(1, pairs * tiles * blocks / SHARE));
     if (p.groups > 8) p.groups &= ~7;
