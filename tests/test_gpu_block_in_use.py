@@ -86,6 +86,19 @@ def test_project_int_is_exact(dtype, M, d, hq, hkv, dh):
     assert torch.equal(out[0], _project_plain(xq[0], sx[0], wq, sw, DT[dtype]))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,d", [(9, 96), (16, 1024), (20, 64), (32, 544), (33, 160), (64, 96)])
+def test_project_int_few_tokens_wide(dtype, M, d):
+    """1023 tiles of 16 weight rows: two or four to a workgroup, the last one short."""
+    test_project_int_is_exact(dtype, M, d, 341, 341, 16)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,d", [(300, 768), (3, 1024), (2, 1056), (1, 2080)])
+def test_quant_rows_of_middle_sizes(dtype, rows, d):
+    test_quant_rows(dtype, rows, d)
+
+
 @pytest.mark.parametrize("M", [3, 100])
 def test_project_int_largest_sums(M):
     """All codes -128 at the largest d_model: sums of 2^14 * 131040 stay in 32 bits."""
@@ -455,6 +468,20 @@ def test_attention_with_a_split_key_axis(dtype, bits, seqs):
 ])
 def test_attention_of_uneven_sequences(dtype, bits, dh, seqs):
     su = Setup(dtype, seqs, 8, 2, dh, bits, rope=10000.0, page=64, spare_rows=1)
+    su.history()
+    y = su.y(su.M, 3.0)
+    jab.cache_write(su.p, su.cache, su.rows, y)
+    _check_attention(su, y)
+
+
+@pytest.mark.parametrize("dtype,bits,dh,seqs", [
+    # prompts without or with a short past: few blocks, many tiles of rows
+    ("bf16", 8, 128, [(0, 300), (0, 17), (100, 256)]), ("f16", 4, 64, [(0, 140), (0, 0), (0, 512)]),
+    ("f32", 8, 16, [(0, 640)]), ("bf16", 4, 64, [(300, 40)]),
+])
+def test_attention_of_short_prompts(dtype, bits, dh, seqs):
+    su = Setup(dtype, seqs, 8, 2, dh, bits, rope=10000.0, page=32, spare_rows=1)
+    assert jab.attn_cache_workspace(su.p, su.cache, su.rows).numel() > 0                 # shares
     su.history()
     y = su.y(su.M, 3.0)
     jab.cache_write(su.p, su.cache, su.rows, y)
