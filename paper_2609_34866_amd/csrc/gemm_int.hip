@@ -207,6 +207,19 @@ __global__ __launch_bounds__(256, 2) void int_small_kernel(IntArgs g) {
         for (int j = 0; j < FB; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+    // the scales, not asked for at the end (6126 x 2304, K 768: 19.5 us with their loads there, 17.8)
+    float sa[FB];
+    f32x4 sb[FB][2][2];
+#pragma unroll
+    for (int i = 0; i < FB; ++i) {
+        sa[i] = g.sa[min(bm0 + wr * (BT / 2) + 32 * i + l32, g.M - 1)];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int col = min(bn0 + wc * (BT / 2) + 32 * i + 16 * p, g.N - 16) + 4 * half;
+            sb[i][p][0] = *reinterpret_cast<const f32x4 *>(g.sb + col);
+            sb[i][p][1] = *reinterpret_cast<const f32x4 *>(g.sb + col + 8);
+        }
+    }
 #pragma unroll
     for (int s0 = 0; s0 < NS - 1; ++s0) issue(s0, s0);
     int slot = 0;
@@ -239,7 +252,7 @@ __global__ __launch_bounds__(256, 2) void int_small_kernel(IntArgs g) {
     for (int i = 0; i < FB; ++i) {
         const int row = bm0 + wr * (BT / 2) + 32 * i + l32;
         if (row >= g.M) continue;
-        const float s = g.sa[row];
+        const float s = sa[i];
         elem *crow = static_cast<elem *>(g.C) + (int64_t)row * g.N;
 #pragma unroll
         for (int j = 0; j < FB; ++j)
@@ -247,8 +260,7 @@ __global__ __launch_bounds__(256, 2) void int_small_kernel(IntArgs g) {
             for (int p = 0; p < 2; ++p) {
                 const int col = bn0 + wc * (BT / 2) + 32 * j + 16 * p;
                 if (col >= g.N) continue;
-                const f32x4 ta = *reinterpret_cast<const f32x4 *>(g.sb + col + 4 * half);
-                const f32x4 tb = *reinterpret_cast<const f32x4 *>(g.sb + col + 8 + 4 * half);
+                const f32x4 ta = sb[j][p][0], tb = sb[j][p][1];
                 const i32x16 &d = acc[i][j];
                 const f32x4 a = scaled4(d[8 * p], d[8 * p + 1], d[8 * p + 2], d[8 * p + 3], s, ta);
                 const f32x4 b = scaled4(d[8 * p + 4], d[8 * p + 5], d[8 * p + 6], d[8 * p + 7], s, tb);
