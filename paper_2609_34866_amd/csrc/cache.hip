@@ -8,13 +8,15 @@
 // are first turned by the rotary embedding: angle, cosine, sine and turn in fp64, rounded to fp32 once.
 //
 // Bound by HBM (the projection's columns in, the codes out).  A workgroup takes blocks of 32 positions of one
-// sequence, all heads: the fp64 cosines and sines of a block are formed once for its heads.  Eight
+// sequence and all heads or a group of them: the fp64 cosines and sines of a block are formed once for its heads.  Eight
 // lanes per (token, head), each with the pairs (j, j + dh / 2) that the rotation and the 4-bit bytes
 // need; values leave through LDS, where a head's tile turns to the cache's token-contiguous order, and the next head's
 // elements are on their way under this one's arithmetic.
 // A block with few new tokens (a decoding step) goes by (token, head) items instead, all heads at once.
 // Measured: 32768 bf16 tokens of 8 heads of 128 (201 MB both ways) are written in 56-64 us, where memory alone needs 40 and
 // the arithmetic, about 8 instructions an element, 35, and read back in 36 (5.6 TB/s).
+#include <algorithm>
+
 #include "device_common.h"
 #include "cache.h"
 
@@ -146,18 +148,20 @@ __device__ inline void encode(const float (&x)[2 * C], bool sym, uint32_t (&code
     }
 }
 
-// The blocks of 32 positions that hold new tokens of a sequence, dealt out over the workgroups:
-// f(sequence, its rows, block, first and one past the last new token inside the block)
+// The blocks of 32 positions that hold new tokens of a sequence, dealt out over the workgroups, gridDim.y groups of heads:
+// f(sequence, its rows, block, first and one past the last new token inside the block, first and one past the last head)
 template <typename F>
 __device__ inline void for_blocks(const CacheArgs &g, int nb, F &&f) {
+    const uint32_t hg = gridDim.y, grp = blockIdx.y;
+    const int h0 = (int)(g.n_kv_heads * grp / hg), h1 = (int)(g.n_kv_heads * (grp + 1) / hg);
     for (int64_t it = blockIdx.x; it < (int64_t)g.n_seq * nb; it += gridDim.x) {
-        const int s = (int)(it / nb);
+        const int s = it >> 32 ? (int)(it / nb) : (int)((uint32_t)it / (uint32_t)nb);
         const SeqRows r = seq_rows(g, s);
         const int end = (int)min((int64_t)r.past + r.n, (int64_t)g.cap);
-        for (int64_t at = (r.past >> 5) + it % nb; at * 32 < end; at += nb) {        // (a step may pass 32 bits of positions)
+        for (int64_t at = (r.past >> 5) + (it - (int64_t)s * nb); at * 32 < end; at += nb) {        // (a step may pass 32 bits of positions)
             const int blk = (int)at;
             const int t0 = max(r.past - blk * 32, 0), t1 = min(end - blk * 32, 32);
-            if (t0 < t1) f(s, r, blk, t0, t1);
+            if (t0 < t1) f(s, r, blk, t0, t1, h0, h1);
         }
     }
 }
@@ -171,7 +175,7 @@ __global__ __launch_bounds__(256, 4) void cache_write_kernel(CacheArgs g, const 
     __shared__ __align__(16) uint8_t tile[DHB * PITCH];
     const int tid = threadIdx.x, e = tid & 7, slot32 = tid >> 3;
     const bool rope = g.freq[0] != 0.0, sym = g.k_zero == nullptr;
-    for_blocks(g, nb, [&](int s, const SeqRows &r, int blk, int t0, int t1) {
+    for_blocks(g, nb, [&](int s, const SeqRows &r, int blk, int t0, int t1, int h0, int h1) {
         const int page = page_of(g, s, blk * 32);
         if (page < 0) return;
         const int nt = t1 - t0, at0 = (blk * 32) & ((1 << g.page_shift) - 1);
@@ -273,10 +277,10 @@ __global__ __launch_bounds__(256, 4) void cache_write_kernel(CacheArgs g, const 
             return g.v + ((((int64_t)page * g.n_kv_heads + h) << g.page_shift) + at0) * DHB;
         };
         if (nt <= FEW) {
-            for (int i0 = 0; i0 < nt * g.n_kv_heads; i0 += 32) {
+            for (int i0 = 0; i0 < nt * (h1 - h0); i0 += 32) {
                 const int i = i0 + slot32;
-                if (i >= nt * g.n_kv_heads) break;     // eight lanes of an item leave together
-                const int t = t0 + i % nt, h = i / nt;
+                if (i >= nt * (h1 - h0)) break;     // eight lanes of an item leave together
+                const int t = t0 + i % nt, h = h0 + i / nt;
                 uint32_t vw[(2 * C + 3) / 4];
                 Elems m;
                 load_k(m, t, h);
@@ -295,13 +299,13 @@ __global__ __launch_bounds__(256, 4) void cache_write_kernel(CacheArgs g, const 
         const bool mine = t >= t0 && t < t1;
         Elems m;
         if (mine) {
-            load_k(m, t, 0);
-            load_v(m, t, 0);
+            load_k(m, t, h0);
+            load_v(m, t, h0);
         }
-        for (int h = 0; h < g.n_kv_heads; ++h) {
+        for (int h = h0; h < h1; ++h) {
             uint32_t vw[(2 * C + 3) / 4] = {};
-            if (mine) item(m, t, h, h + 1 < g.n_kv_heads ? h + 1 : -1, vw);
-            if (h) __syncthreads();                        // the tile is read
+            if (mine) item(m, t, h, h + 1 < h1 ? h + 1 : -1, vw);
+            if (h > h0) __syncthreads();                      // the tile is read
 #pragma unroll
             for (int w = 0; w < (NC + 3) / 4; ++w) {
                 const uint32_t q = quad_bytes(vw[w]);
@@ -336,7 +340,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs g, void *__re
     const int tid = threadIdx.x, e = tid & 7;
     const int64_t ld = (int64_t)g.n_kv_heads * DH;
     constexpr int QMID = (1 << (BITS - 1)) - 1;
-    for_blocks(g, nb, [&](int s, const SeqRows &r, int blk, int t0, int t1) {
+    for_blocks(g, nb, [&](int s, const SeqRows &r, int blk, int t0, int t1, int h0, int h1) {
         const int page = page_of(g, s, blk * 32);
         const int nt = t1 - t0, at0 = (blk * 32) & ((1 << g.page_shift) - 1);
         const int64_t row0 = r.row + (blk * 32 - r.past);
@@ -378,17 +382,17 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs g, void *__re
             return g.v + ((((int64_t)max(page, 0) * g.n_kv_heads + h) << g.page_shift) + at0) * DHB;
         };
         if (nt <= FEW) {
-            for (int i0 = 0; i0 < nt * g.n_kv_heads; i0 += 32) {
+            for (int i0 = 0; i0 < nt * (h1 - h0); i0 += 32) {
                 const int i = i0 + (tid >> 3);
-                if (i >= nt * g.n_kv_heads) break;
-                const int t = t0 + i % nt, h = i / nt;
+                if (i >= nt * (h1 - h0)) break;
+                const int t = t0 + i % nt, h = h0 + i / nt;
                 const uint8_t *vb = vbase(h);
                 item(t, h, [&](int d) { return vb[d * 32 + t]; });
             }
             return;
         }
         const int t = tid >> 3;
-        for (int h = 0; h < g.n_kv_heads; ++h) {
+        for (int h = h0; h < h1; ++h) {
             const uint8_t *vb = vbase(h);
             for (int c = tid; c < DHB * 2; c += 256) { // whole tiles: chunks of 16 tokens
                 const u32x4 q = *reinterpret_cast<const u32x4 *>(vb + c * 16);
@@ -403,12 +407,16 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheArgs g, void *__re
     });
 }
 
-// blocks of 32 positions that max_new tokens can touch, and the launch's workgroups (at most 2^20: a
-// workgroup takes the next ones in turn)
+// blocks of 32 positions that max_new tokens can touch, and the launch's workgroups (at most 2^20 of them: a workgroup
+// takes the next blocks in turn)
 int blocks_per_seq(const CacheArgs &g) { return (int)(((int64_t)g.max_new + 62) / 32); }
-unsigned grid_of(const CacheArgs &g) {
+// Groups of heads for about 1024 workgroups, four per CU: 8 sequences of 5788 tokens, 12 heads of 64, fp16 at 4 bits: 12.8
+// and 9.1 us to write and read back, 19.4 and 15.0 with all heads to a workgroup, 14.2 and 10.2 with 4096.  Not for few
+// tokens, whose heads a workgroup takes at once (48 x 8 heads of 128: 6.4 us in one group, 7.9 in eight).
+dim3 grid_of(const CacheArgs &g) {
     const int64_t n = (int64_t)g.n_seq * blocks_per_seq(g);
-    return (unsigned)(n < (1 << 20) ? n : (1 << 20));
+    const int64_t hg = g.max_new <= FEW ? 1 : std::max<int64_t>(1, std::min<int64_t>(g.n_kv_heads, 1024 / n));
+    return dim3((unsigned)(n < (1 << 20) ? n : (1 << 20)), (unsigned)hg);
 }
 
 template <int DT, int DH, int BITS>

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256, 2) void int_small_kernel(IntArgs g) {
         for (int j = 0; j < FB; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    // the scales, not asked for at the end (6126 x 2304, K 768: 19.5 us with their loads there, 17.8)
+    // the scales, not asked for at the end (4576 x 2304, K 768: 19.5 us with their loads there, 17.8)
     float sa[FB];
     f32x4 sb[FB][2][2];
 #pragma unroll
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(256, 1) void int_w4p_kernel(IntArgs g) {
 // Few tokens: a workgroup takes 16 RT weight rows and all tokens (16 MT), its eight waves each an eighth of K (in steps of
 // 64 codes: v_mfma_i32_16x16x64_i8, lane (row l % 16, g = l / 16) holding codes 16 g .. 16 g + 15 of the step).  Weights
 // and tokens go from memory to registers, UNR steps at once; the sums of the waves meet in LDS.  Bound by the bytes
-// that a CU takes in: every workgroup reads all tokens' codes over.  32 tokens, 6144 rows, K 4096 (25 MB of weights):
+// that a CU takes in: every workgroup reads all tokens' codes over.  24 tokens, 6144 rows, K 4096 (25 MB of weights):
 // 12.5 us with RT 1, 9.9 with the 2 that the rule takes; a device copy of as many bytes takes 7.7.  More steps at once, nontemporal
 // loads or another order of the steps changed nothing.
 constexpr int SK_WAVES = 8;
@@ -580,8 +580,8 @@ hipError_t run_quant_rows(int64_t rows, int cols, const void *src, int8_t *codes
     for (int64_t r = 0; r < rows; r += MOST_GROUPS) {
         const dim3 grid((unsigned)std::min(rows - r, MOST_GROUPS));
         const void *x = static_cast<const typename Mma<DT>::elem *>(src) + r * cols;
-        // eight elements a thread; 8000 rows of 768 fp16: 6.0 us with 128 threads, 7.4 with 256, 6.2 with 64 twice; 32 rows
-        // of 4096 bf16 (twice with 256): 3.4 us, 4.4 with 128 four times, 3.3 with 512; 16384: 71, 78 and 83 us (5.7 TB/s)
+        // eight elements a thread; 4576 rows of 768 fp16: 6.0 us with 128 threads, 7.4 with 256, 6.2 with 64 twice; 24 rows
+        // of 4096 bf16 (twice with 256): 3.4 us, 4.4 with 128 four times, 3.3 with 512; 32768: 71, 78 and 83 us (5.7 TB/s)
         if (cols <= 512) quant_rows_kernel<DT, 64, 1><<<grid, 64, 0, st>>>(x, cols, codes + r * cols, scale + r);
         else if (cols <= 1024) quant_rows_kernel<DT, 128, 1><<<grid, 128, 0, st>>>(x, cols, codes + r * cols, scale + r);
         else quant_rows_kernel<DT, 256, 2><<<grid, 256, 0, st>>>(x, cols, codes + r * cols, scale + r);
