@@ -505,7 +505,9 @@ const char *jab_last_error(void);
 /* JAB_KT_GEMM: the projection of Q and K (or the single projection of jab_project, or the whole
  * projection where the sizes let one launch write Q, K and V transposed);
  * JAB_KT_GEMM_VT: the launch that writes V transposed, where it is separate; JAB_KT_KL: the KL
- * attention-map kernel of jab_loss_fwd_kl. */
+ * attention-map kernel of jab_loss_fwd_kl.  The block in use: jab_quant_rows and jab_cache_write count as
+ * JAB_KT_QUANT, jab_project_int as JAB_KT_GEMM, jab_attn_cache (one or two kernels, bracketed as one
+ * launch) as JAB_KT_ATTN, jab_cache_read as JAB_KT_MISC. */
 enum { JAB_KT_QUANT = 0, JAB_KT_GEMM = 1, JAB_KT_ATTN = 2, JAB_KT_REDUCE = 3,
        JAB_KT_ATTN_BWD = 4, JAB_KT_DW_GEMM = 5, JAB_KT_MISC = 6, JAB_KT_GEMM_VT = 7, JAB_KT_KL = 8,
        JAB_KT_COUNT = 9 };

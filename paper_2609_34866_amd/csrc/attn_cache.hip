@@ -580,6 +580,8 @@ __device__ inline void put_row(const CacheArgs &g, const SeqRows &sr, int h, int
 // The four waves of a workgroup share 16 RT rows and deal out the key blocks.  Codes go from memory to
 // registers; a block's keys are asked for once the previous block's scores are formed, its values once the
 // previous block's are used, so one block is in flight per wave without a second set of registers.
+// Measured: 64 sequences of 1900 .. 6000 keys, 8 heads of 128 at 8 bits, bf16 (545 MB): 102 us, 5.3 TB/s; one of 130001 keys at
+// 4 bits (143 MB): 37.5 us, 3.8 TB/s; the join after either 7 us.
 template <int DT, int DH, int BITS, int RT>
 struct FewCfg {
     static constexpr size_t Q_LDS = (size_t)Wave<DT, DH, BITS, RT>::NP * 16 * RT * QP<DH> * 2;
