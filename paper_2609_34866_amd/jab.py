@@ -400,6 +400,7 @@ def loss_bwd_kl(p: Problem, x, w, bits, scale, zero, a_ref, qk_ref, lse_ref, gsc
 # --------------------------------------------------------------------------- the block in use
 # A decoding step is a few microseconds on the device, so these calls keep what the host does short: the tensors'
 # dtype, shape, layout and device are checked here, everything else in the library.
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
@@ -407,7 +408,7 @@ def _here(t: torch.Tensor) -> int:
     """The current GPU, on which the call's tensors have to be (t: one of them)."""
     if not t.is_cuda:
         raise JabError(JAB_E_INVALID, f"a tensor is on {t.device}, not on the current GPU")
-    return torch.cuda.current_device()
+    return _current()
 
 
 def _stream_of(dev: int) -> int:
@@ -435,10 +436,15 @@ def quant_rows(p: Problem, src: torch.Tensor, codes: Optional[torch.Tensor] = No
     sp = _arg("src", src, _CODE_DTYPE[p.dtype], shape, dev)
     if codes is None:
         codes = torch.empty_like(src, dtype=torch.int8)
+        cp = codes.data_ptr()
+    else:
+        cp = _arg("codes", codes, torch.int8, shape, dev)
     if scale is None:
         scale = src.new_empty(shape[:-1], dtype=torch.float32)
-    _check(lib().jab_quant_rows(ctypes.byref(p), src.numel() // d, sp, _arg("codes", codes, torch.int8, shape, dev),
-                                _arg("scale", scale, torch.float32, shape[:-1], dev), _stream_of(dev)))
+        ap = scale.data_ptr()
+    else:
+        ap = _arg("scale", scale, torch.float32, shape[:-1], dev)
+    _check(lib().jab_quant_rows(ctypes.byref(p), src.numel() // d, sp, cp, ap, _stream_of(dev)))
     return codes, scale
 
 
@@ -449,10 +455,12 @@ def project_int(p: Problem, xq: torch.Tensor, sx: torch.Tensor, wq: torch.Tensor
     B, T, d, R, dt, dev = p.batch, p.seq_len, p.d_model, p.rows, _CODE_DTYPE[p.dtype], _here(xq)
     if out is None:
         out = xq.new_empty((B, T, R), dtype=dt)
+        yp = out.data_ptr()
+    else:
+        yp = _arg("out", out, dt, (B, T, R), dev)
     _check(lib().jab_project_int(ctypes.byref(p), _arg("xq", xq, torch.int8, (B, T, d), dev),
                                  _arg("sx", sx, torch.float32, (B, T), dev), _arg("wq", wq, torch.int8, (R, d), dev),
-                                 _arg("sw", sw, torch.float32, (R,), dev), _arg("out", out, dt, (B, T, R), dev),
-                                 _stream_of(dev)))
+                                 _arg("sw", sw, torch.float32, (R,), dev), yp, _stream_of(dev)))
     return out
 
 
@@ -517,7 +525,7 @@ def _cache_call(p: Problem, cache: Cache, rows: CacheRows) -> int:
     """The GPU of a call on this cache and these rows."""
     if cache.geometry != (p.n_kv_heads, p.head_dim, p.scheme):
         raise JabError(JAB_E_INVALID, "the cache was laid out for other heads or another scheme")
-    dev = torch.cuda.current_device()
+    dev = _current()
     if cache.device != dev or rows.device != dev:
         raise JabError(JAB_E_INVALID, "the cache and its rows must be on the current GPU")
     return dev
@@ -536,10 +544,15 @@ def cache_read(p: Problem, cache: Cache, rows: CacheRows, k: Optional[torch.Tens
     dev, dt, shape = _cache_call(p, cache, rows), _CODE_DTYPE[p.dtype], (p.batch, p.seq_len, p.n_kv_heads * p.head_dim)
     if k is None:
         k = cache.tensors[0].new_empty(shape, dtype=dt)
+        kp = k.data_ptr()
+    else:
+        kp = _arg("k", k, dt, shape, dev)
     if v is None:
         v = cache.tensors[0].new_empty(shape, dtype=dt)
-    _check(lib().jab_cache_read(ctypes.byref(p), cache.ref, rows.ref, _arg("k", k, dt, shape, dev),
-                                _arg("v", v, dt, shape, dev), _stream_of(dev)))
+        vp = v.data_ptr()
+    else:
+        vp = _arg("v", v, dt, shape, dev)
+    _check(lib().jab_cache_read(ctypes.byref(p), cache.ref, rows.ref, kp, vp, _stream_of(dev)))
     return k, v
 
 
@@ -556,13 +569,16 @@ def attn_cache(p: Problem, cache: Cache, rows: CacheRows, y: torch.Tensor, ws: O
     """Attention of y's query columns over the cache -> [B][T][n_heads * head_dim] in the dtype."""
     dev, dt, B, T = _cache_call(p, cache, rows), _CODE_DTYPE[p.dtype], p.batch, p.seq_len
     shape = (B, T, p.n_heads * p.head_dim)
+    yp = _arg("y", y, dt, (B, T, p.rows), dev)
     if out is None:
         out = y.new_empty(shape)
+        ap = out.data_ptr()
+    else:
+        ap = _arg("out", out, dt, shape, dev)
     if ws is None:
         ws = attn_cache_workspace(p, cache, rows)
-    _check(lib().jab_attn_cache(ctypes.byref(p), cache.ref, rows.ref, _arg("y", y, dt, (B, T, p.rows), dev),
-                                _arg("out", out, dt, shape, dev), _arg("ws", ws, torch.uint8, ws.shape, dev), ws.numel(),
-                                _stream_of(dev)))
+    _check(lib().jab_attn_cache(ctypes.byref(p), cache.ref, rows.ref, yp, ap, _arg("ws", ws, torch.uint8, ws.shape, dev),
+                                ws.numel(), _stream_of(dev)))
     return out
 
 
