@@ -643,6 +643,25 @@ def test_block_from_tokens_to_attention():
 
 
 # ------------------------------------------------------------------ streams and graphs
+@pytest.mark.parametrize("bits,seqs", [(8, [(700, 1), (90, 2)]), (4, [(300, 70), (0, 33)])])
+def test_pages_behind_4_gib(bits, seqs):
+    """The same pages at the front of a small cache and behind 2^32 bytes of codes: bitwise the same results."""
+    got = []
+    for big in (False, True):
+        su = Setup("bf16", seqs, 8, 2, 128, bits, rope=10000.0, page=256, spare_rows=0)
+        if big:
+            n = (1 << 32) // (256 * 2 * 128 * bits // 8)
+            used = su.cache.tensors[0].shape[0]
+            su.cache = jab.Cache.empty(su.p, bits, 256, n + used)
+            su.pages += torch.where(su.pages >= 0, n, 0).to(torch.int32)
+        su.history()
+        y = su.y(su.M, 3.0)
+        jab.cache_write(su.p, su.cache, su.rows, y)
+        got.append(jab.cache_read(su.p, su.cache, su.rows) + (jab.attn_cache(su.p, su.cache, su.rows, y),))
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 def test_another_stream_and_repeats():
     su = Setup("bf16", [(700, 1), (33, 1)], 8, 2, 128, page=64, spare_rows=0)
     su.history()
