@@ -427,7 +427,9 @@ __device__ inline void store4(typename Mma<DT>::elem *p, f32x4 v) {
 // A cut closer than SNAP blocks to a tile's end moves there.  A tile that lies in one share is written as output;
 // a share has at most two pieces of others, its first (slot 0: the tile began in an earlier share) and its last (slot 1:
 // the tile begins here), which attn_join_kernel joins.
-constexpr int SNAP = 8, SHARE = 8;      // least blocks of a piece, of a share
+constexpr int SNAP = 8, SHARE = 8;      // least blocks of a piece, of a share (4 for either or both: 1 x 940 rows on 34892
+                                        // keys 194 .. 223 us for 203, 2 x 2048 on 512 43 .. 53 for 50, 8 x 512 on 528 42 .. 50
+                                        // for 39, single tokens the same)
 constexpr int SCAN_SEQS = 512;          // sequences up to which each workgroup scans them; past it one workgroup per
                                         // (sequence, head), of which there are then enough (1024 x 8 of 1600 tokens: 581 us,
                                         // 634 with shares; 512: 285 and 313, but uneven lengths want them)
