@@ -10,7 +10,7 @@
 //    blocks of v_mfma_i32_32x32x32_i8; the LDS rings, refills and waits of gemm_w4p_kernel (gemm.hip), whose
 //    16-byte chunks hold 16 codes here instead of 8 values, at twice the product rate per byte.
 //  * int_small_kernel: 128 x 128 or 64 x 64 tiles for the shapes whose 256-tiles leave CUs idle.
-//  * int_skinny_kernel: up to 64 tokens.  The weights are what is read: each wave streams 16 weight
+//  * int_skinny_kernel: up to 32 tokens.  The weights are what is read: each wave streams 16, 32 or 64 weight
 //    rows straight into registers, the waves of a workgroup share K, their sums meet in LDS.
 #include <algorithm>
 
@@ -543,21 +543,25 @@ hipError_t run_skinny(IntArgs a, hipStream_t st) {
     auto groups = [&](int rt) { return (tiles + rt - 1) / rt; };
     auto cost = [&](int rt) { return (int64_t)((groups(rt) + CUS - 1) / CUS) * (rt + MT); };
     int rt = cost(2) < cost(1) ? 2 : 1;
-    if (MT <= 2 && cost(4) < cost(rt)) rt = 4;
+    if (cost(4) < cost(rt)) rt = 4;
     if (rt == 1) int_skinny_kernel<DT, 1, MT><<<groups(1), 64 * SK_WAVES, 0, st>>>(a);
     else if (rt == 2) int_skinny_kernel<DT, 2, MT><<<groups(2), 64 * SK_WAVES, 0, st>>>(a);
-    else if constexpr (MT <= 2) int_skinny_kernel<DT, 4, MT><<<groups(4), 64 * SK_WAVES, 0, st>>>(a);
+    else int_skinny_kernel<DT, 4, MT><<<groups(4), 64 * SK_WAVES, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <int DT>
 hipError_t run_int(IntArgs a, hipStream_t st) {
-    if (a.M <= 16) return run_skinny<DT, 1>(a, st);
-    if (a.M <= 32) return run_skinny<DT, 2>(a, st);
-    if (a.M <= 64) return run_skinny<DT, 4>(a, st);
+    // Few tokens where 64-tiles leave CUs idle (bf16; this / 64-tiles): 1 token 6144 x 4096 7.0 / 10.9 us, 24 tokens 9.6 / 10.9,
+    // 6144 x 16384 30 / 34; not 64 tokens (14.3 / 11.1), 32 of 2304 x 768 (5.2 / 4.5), 32 of 24576 x 4096 (26 / 17.5)
+    if ((a.N + 63) / 64 <= CUS) {
+        if (a.M <= 16) return run_skinny<DT, 1>(a, st);
+        if (a.M <= 32 && a.K >= 1024) return run_skinny<DT, 2>(a, st);
+    }
     const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256, t = tm * tn;
-    // the 256-tiles where they fill their rounds of one workgroup per CU to at least 70 %
-    if (a.M >= 256 && a.N >= 256 && a.K % 128 == 0 && a.K >= 1024 && 10 * t >= 7 * ((t + CUS - 1) / CUS) * CUS) {
+    // the 256-tiles where they fill their rounds of one workgroup per CU to at least 60 % (bf16, K 4096; 128-tiles / these:
+    // 66 % 57.9 / 52.6 and 105 / 97.5 us, 75 % 63.6 / 61.8, 94 % 77.5 / 58.7; but 47 % 38.0 / 47.2, and 56 % at K 1024 30.6 / 34.4)
+    if (a.M >= 256 && a.N >= 256 && a.K % 128 == 0 && a.K >= 1024 && 10 * t >= 6 * ((t + CUS - 1) / CUS) * CUS) {
         constexpr size_t LDS = 5 * 256 * 128;
         a.tiles_m = (int)tm;
         a.tiles_n = (int)tn;
@@ -567,7 +571,9 @@ hipError_t run_int(IntArgs a, hipStream_t st) {
         int_w4p_kernel<DT><<<dim3((unsigned)std::min<int64_t>(t, CUS)), 256, LDS, st>>>(a);
         return hipGetLastError();
     }
-    const bool big = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128) >= CUS;
+    // 128-tiles where they occupy three quarters of the CUs (K 4096; 64-tiles / these: 96 tiles 14.9 / 21.6 us, 192 24.5 / 24.0,
+    // 240 30.3 / 24.7, 384 43.2 / 34.5)
+    const bool big = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128) >= CUS * 3 / 4;
     if (a.K % 128 == 0) return big ? run_small<DT, 128, 8>(a, st) : run_small<DT, 64, 8>(a, st);
     if (a.K % 64 == 0) return big ? run_small<DT, 128, 4>(a, st) : run_small<DT, 64, 4>(a, st);
     return big ? run_small<DT, 128, 2>(a, st) : run_small<DT, 64, 2>(a, st);

@@ -87,10 +87,11 @@ def test_project_int_is_exact(dtype, M, d, hq, hkv, dh):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,d", [(9, 96), (16, 1024), (20, 64), (32, 544), (33, 160), (64, 96)])
+@pytest.mark.parametrize("M,d", [(9, 96), (16, 1024), (20, 64), (20, 1056), (32, 2048), (32, 544), (33, 160), (64, 96)])
 def test_project_int_few_tokens_wide(dtype, M, d):
-    """1023 tiles of 16 weight rows: two or four to a workgroup, the last one short."""
+    """1023 tiles of 16 weight rows: four to a workgroup, the last one short; 513: two."""
     test_project_int_is_exact(dtype, M, d, 341, 341, 16)
+    test_project_int_is_exact(dtype, M, d, 171, 171, 16)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
